@@ -16,7 +16,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIBDIR = os.path.join(HERE, "lib")
 LIBNAME = "libcompresskv.so"
 SOURCES = ["api.hip", "score_kernels.hip", "score_layers.hip", "onepass_score.hip",
-           "select_gather_kernels.hip", "offline.hip", "decode_error.hip"]
+           "select_gather_kernels.hip", "offline.hip", "decode_error.hip", "cache.hip",
+           "attend.hip", "attend_fp4.hip", "attend_bf16.hip", "attend_f32.hip",
+           "window_attention.hip"]
 ARCH = "gfx950"
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++20", "-fPIC",
@@ -42,12 +44,15 @@ def _hipcc() -> str:
     return p
 
 
-# Per-source additions.  The two-pass scoring kernels keep MFMA results in
-# VGPRs, where the softmax arithmetic reads them (the single-pass kernel is
+# Per-source additions.  The two-pass scoring kernels and the attention keep
+# MFMA results in VGPRs, where the softmax arithmetic reads them (the single-pass kernel is
 # left to the default heuristics: this compiler fails on it with the option).
 EXTRA = {
     "score_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "score_layers.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "attend_fp4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "attend_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "attend_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 

@@ -1,12 +1,13 @@
 """Python binding of libcompresskv (ctypes; argument marshalling only).
 
-The functions mirror the C ABI in include/compresskv.h and
-include/compresskv_offline.h and take torch tensors
-for device memory; every computation runs in the HIP library.  There is no
+The functions mirror the C ABI in include/compresskv.h,
+include/compresskv_offline.h and include/compresskv_cache.h and take torch
+tensors for device memory; every computation runs in the HIP library.  There is no
 fallback: if the library is missing or fails to load, every call raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -18,7 +19,7 @@ import torch
 from . import build as _build
 
 OK, INVALID_ARGUMENT, UNSUPPORTED, WORKSPACE_TOO_SMALL, HIP_ERROR = 0, 1, 2, 3, 4
-F32, BF16 = 0, 1
+F32, BF16, FP4 = 0, 1, 2
 POOL_MAX, POOL_AVG = 0, 1
 POOL_THEN_MEAN, MEAN_THEN_POOL = 0, 1
 INDEX_PER_GROUP, INDEX_LAYER = 0, 1
@@ -26,7 +27,8 @@ SCORE_AUTO, SCORE_TWO_PASS, SCORE_ONE_PASS, SCORE_TWO_LAUNCHES = 0, 1, 2, 3
 SPIN_DEFAULT, SPIN_CATCHUP_ALL = -1, -2
 
 _INCLUDE = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
-_HEADERS = [os.path.join(_INCLUDE, h) for h in ("compresskv.h", "compresskv_offline.h")]
+_HEADERS = [os.path.join(_INCLUDE, h) for h in ("compresskv.h", "compresskv_offline.h",
+                                                "compresskv_cache.h")]
 
 
 class CkvProblem(ctypes.Structure):
@@ -70,6 +72,59 @@ class CkvErrorProblem(ctypes.Structure):
         ("d_model", ctypes.c_int32),
         ("budget", ctypes.c_int32),
         ("eps", ctypes.c_float),
+    ]
+
+
+class CkvCache(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("capacity", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("pos", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p),
+        ("len", ctypes.c_void_p),
+        ("seen", ctypes.c_void_p),
+    ]
+
+
+class CkvAttendProblem(ctypes.Structure):
+    _fields_ = [
+        ("n_q_heads", ctypes.c_int32),
+        ("n_q", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("accumulate", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class CkvWindowProblem(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("n_q_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("window", ctypes.c_int32),
+        ("n_sinks", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("cu_q", ctypes.c_void_p),
+        ("cu_q_host", ctypes.c_void_p),
+        ("cu_k", ctypes.c_void_p),
+        ("cu_k_host", ctypes.c_void_p),
+        ("q_stride_tok", ctypes.c_int64),
+        ("q_stride_head", ctypes.c_int64),
+        ("k_stride_tok", ctypes.c_int64),
+        ("k_stride_head", ctypes.c_int64),
+        ("v_stride_tok", ctypes.c_int64),
+        ("v_stride_head", ctypes.c_int64),
     ]
 
 
@@ -137,6 +192,24 @@ def lib() -> ctypes.CDLL:
     L.compresskv_layer_error.restype = ctypes.c_int
     L.compresskv_allocate_budgets.argtypes = [i32, vp, ctypes.c_int64, i32, i32, vp]
     L.compresskv_allocate_budgets.restype = ctypes.c_int
+    CP, AP = ctypes.POINTER(CkvCache), ctypes.POINTER(CkvAttendProblem)
+    WP = ctypes.POINTER(CkvWindowProblem)
+    L.compresskv_cache_load.argtypes = [CP, i32, i32, vp, vp, vp, vp, vp, vp]
+    L.compresskv_cache_append.argtypes = [CP, i32, i32, vp, vp, vp, vp, vp]
+    L.compresskv_cache_read.argtypes = [CP, i32, vp, vp, vp]
+    L.compresskv_cache_attend.argtypes = [CP, AP, vp, vp, vp, sz, vp]
+    L.compresskv_cache_evict.argtypes = [CP, i32, i32, i32, vp, sz, vp]
+    L.compresskv_window_attention.argtypes = [WP, vp, vp, vp, vp, vp, sz, vp]
+    for f in ("compresskv_cache_load", "compresskv_cache_append", "compresskv_cache_read",
+              "compresskv_cache_attend", "compresskv_cache_evict",
+              "compresskv_window_attention"):
+        getattr(L, f).restype = ctypes.c_int
+    L.compresskv_cache_attend_workspace_bytes.argtypes = [CP, AP]
+    L.compresskv_cache_evict_workspace_bytes.argtypes = [CP, i32]
+    L.compresskv_window_attention_workspace_bytes.argtypes = [WP]
+    for f in ("compresskv_cache_attend_workspace_bytes", "compresskv_cache_evict_workspace_bytes",
+              "compresskv_window_attention_workspace_bytes"):
+        getattr(L, f).restype = sz
     _LIB = L
     return L
 
@@ -566,3 +639,283 @@ def compress_layer_heads(p: Problem, q_win, k, v, srh_mask, group_budgets, *, wa
                _ptr(idx), _ptr(k_out), _ptr(v_out), _ptr(scores), _ptr(ws),
                ws.numel() * ws.element_size(), _stream(stream)))
     return idx, k_out, v_out, scores
+
+
+# ---------------------------------------------------------------------------
+# The bounded cache and the windowed attention (include/compresskv_cache.h)
+# ---------------------------------------------------------------------------
+def _enter(device: torch.device, stream):
+    """(context, stream handle) of a call on the tensors' device: temporaries and
+    outputs are allocated on the stream that the call runs on."""
+    if stream is None:
+        here = torch.cuda.current_device() == device.index
+        return (contextlib.nullcontext() if here else torch.cuda.device(device),
+                torch.cuda.current_stream(device).cuda_stream)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
+    return torch.cuda.stream(stream), stream.cuda_stream
+
+
+def _check_tensor(t, name: str, shape, dtype, device) -> None:
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} (got {t.dtype} {tuple(t.shape)})")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+
+
+def _check_on_gpu(device: torch.device) -> None:
+    if device.type != "cuda":
+        raise ValueError(f"the tensors must be on a GPU (got {device})")
+
+
+def _row_dtype(dtype: torch.dtype) -> int:
+    if dtype not in _DTYPES:
+        raise ValueError(f"rows and queries are bfloat16 or float32 (got {dtype})")
+    return _DTYPES[dtype]
+
+
+class Cache:
+    """A layer's bounded KV cache (ckv_cache) over caller-owned tensors:
+
+    k, v [batch, Hkv, capacity, D] (bfloat16 or float32), or for a 4-bit cache
+    uint8 codes [batch, Hkv, capacity, D / 2] with uint8 scales k_scale, v_scale
+    [batch, Hkv, capacity, D / 32]; pos int32 and weight float32 [batch, Hkv,
+    capacity]; length and seen int32 [batch, Hkv].  All contiguous, on one GPU.
+    """
+
+    def __init__(self, k, v, k_scale, v_scale, pos, weight, length, seen):
+        fp4 = k_scale is not None
+        if k.dim() != 4:
+            raise ValueError("k must have four dimensions")
+        b, h, cap, w = k.shape
+        dev = k.device
+        self.batch, self.n_kv_heads, self.capacity = b, h, cap
+        self.head_dim = 2 * w if fp4 else w
+        dtype = torch.uint8 if fp4 else k.dtype
+        if not fp4:
+            _row_dtype(dtype)
+        if fp4 != (v_scale is not None):
+            raise ValueError("k_scale and v_scale come together (a 4-bit cache) or not at all")
+        _check_tensor(k, "k", k.shape, dtype, dev)
+        _check_tensor(v, "v", k.shape, dtype, dev)
+        if fp4:
+            shape = torch.Size((b, h, cap, self.head_dim // 32))
+            _check_tensor(k_scale, "k_scale", shape, torch.uint8, dev)
+            _check_tensor(v_scale, "v_scale", shape, torch.uint8, dev)
+        _check_tensor(pos, "pos", k.shape[:3], torch.int32, dev)
+        _check_tensor(weight, "weight", k.shape[:3], torch.float32, dev)
+        _check_tensor(length, "length", k.shape[:2], torch.int32, dev)
+        _check_tensor(seen, "seen", k.shape[:2], torch.int32, dev)
+        _check_on_gpu(dev)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pos, self.weight, self.length, self.seen = pos, weight, length, seen
+        self.device, self.dtype = dev, (FP4 if fp4 else _DTYPES[dtype])
+        self.c = CkvCache(batch=b, n_kv_heads=h, head_dim=self.head_dim, capacity=cap,
+                          dtype=self.dtype, reserved=0, k=_ptr(k), v=_ptr(v),
+                          k_scale=_ptr(k_scale), v_scale=_ptr(v_scale), pos=_ptr(pos),
+                          weight=_ptr(weight), len=_ptr(length), seen=_ptr(seen))
+        self._ref = ctypes.byref(self.c)
+        self._attends, self._evict_bytes = {}, {}
+
+    @classmethod
+    def empty(cls, batch: int, n_kv_heads: int, capacity: int, head_dim: int, dtype,
+              device) -> "Cache":
+        """A cache without live slots.  dtype: torch.bfloat16, torch.float32 or FP4 (the
+        capacity is then rounded up to a multiple of 32)."""
+        fp4 = dtype == FP4
+        if fp4:
+            capacity = -(-capacity // 32) * 32
+        shape = (batch, n_kv_heads, capacity)
+
+        def new(last, t):
+            return torch.zeros(shape + last, dtype=t, device=device)
+        rows = [new((head_dim // 2,), torch.uint8) if fp4 else new((head_dim,), dtype)
+                for _ in range(2)]
+        scales = [new((head_dim // 32,), torch.uint8) if fp4 else None for _ in range(2)]
+        counts = [torch.zeros(shape[:2], dtype=torch.int32, device=device) for _ in range(2)]
+        return cls(*rows, *scales, torch.full(shape, -1, dtype=torch.int32, device=device),
+                   new((), torch.float32), *counts)
+
+    def load(self, k_rows, v_rows, idx, cu_seqlens, group_budgets=None, stream=None) -> None:
+        """Kept rows of compress_layer (k_out, v_out [batch, Hkv, n, D], idx [batch, Hkv, n]),
+        or with group_budgets of compress_layer_heads ([batch, total, D], [batch, total])."""
+        b, h, d = self.batch, self.n_kv_heads, self.head_dim
+        dtype = _row_dtype(k_rows.dtype)
+        gb = None
+        if group_budgets is None:
+            if idx.dim() != 3:
+                raise ValueError("idx must be [batch, Hkv, n]")
+            n = idx.shape[2]
+            shape = torch.Size((b, h, n))
+        else:
+            gb = _budgets(group_budgets)
+            if gb.shape != (h,):
+                raise ValueError("group_budgets must have one entry per KV group")
+            n = 0
+            shape = torch.Size((b, int(gb.sum())))
+        _check_tensor(idx, "idx", shape, torch.int32, self.device)
+        _check_tensor(k_rows, "k_rows", shape + (d,), k_rows.dtype, self.device)
+        _check_tensor(v_rows, "v_rows", shape + (d,), k_rows.dtype, self.device)
+        _check_tensor(cu_seqlens, "cu_seqlens", torch.Size((b + 1,)), torch.int32, self.device)
+        ctx, handle = _enter(self.device, stream)
+        with ctx:
+            _check("compresskv_cache_load", lib().compresskv_cache_load(
+                self._ref, dtype, n, _ptr(k_rows), _ptr(v_rows), _ptr(idx), _ptr(gb),
+                _ptr(cu_seqlens), handle))
+
+    def append(self, k_new, v_new, stream=None) -> None:
+        """New tokens' rows [batch, n, Hkv, D], D contiguous."""
+        for t, name in ((k_new, "k_new"), (v_new, "v_new")):
+            if (t.dim() != 4 or t.shape[0] != self.batch or t.shape[2] != self.n_kv_heads
+                    or t.shape[3] != self.head_dim or t.shape != k_new.shape):
+                raise ValueError(f"{name} must be [batch, n, Hkv, D]")
+            if t.dtype != k_new.dtype:
+                raise ValueError("k_new and v_new must share one dtype")
+            if t.stride(3) != 1:
+                raise ValueError(f"the head dimension of {name} must be contiguous")
+            if t.device != self.device:
+                raise ValueError(f"{name} must be on {self.device}")
+        strides = [(ctypes.c_int64 * 3)(*t.stride()[:3]) for t in (k_new, v_new)]
+        ctx, handle = _enter(self.device, stream)
+        with ctx:
+            _check("compresskv_cache_append", lib().compresskv_cache_append(
+                self._ref, _row_dtype(k_new.dtype), k_new.shape[1], k_new.data_ptr(), strides[0],
+                v_new.data_ptr(), strides[1], handle))
+
+    def read(self, dtype: torch.dtype | None = None, stream=None):
+        """(k, v) [batch, Hkv, capacity, D] as values, zeros past the live slots."""
+        if dtype is None:
+            dtype = torch.bfloat16 if self.dtype == FP4 else self.k.dtype
+        code = _row_dtype(dtype)
+        shape = (self.batch, self.n_kv_heads, self.capacity, self.head_dim)
+        ctx, handle = _enter(self.device, stream)
+        with ctx:
+            k = torch.empty(shape, dtype=dtype, device=self.device)
+            v = torch.empty(shape, dtype=dtype, device=self.device)
+            _check("compresskv_cache_read", lib().compresskv_cache_read(
+                self._ref, code, k.data_ptr(), v.data_ptr(), handle))
+        return k, v
+
+    def attend(self, q, *, scale: float | None = None, accumulate: bool = False, out=None,
+               ws=None, stream=None):
+        """Attention of q [batch, n_q, Hq, D] over the live slots; returns out, like q.
+        accumulate adds what every slot received to its weight."""
+        if q.dim() != 4 or q.shape[0] != self.batch or q.shape[3] != self.head_dim:
+            raise ValueError("q must be [batch, n_q, Hq, D]")
+        _check_tensor(q, "q", q.shape, q.dtype, self.device)
+        if out is not None:
+            _check_tensor(out, "out", q.shape, q.dtype, self.device)
+        key = (q.shape[1], q.shape[2], q.dtype, bool(accumulate), scale)
+        known = self._attends.get(key)
+        if known is None:
+            a = CkvAttendProblem(n_q_heads=q.shape[2], n_q=q.shape[1], dtype=_row_dtype(q.dtype),
+                                 accumulate=int(bool(accumulate)),
+                                 scale=float(scale) if scale else 0.0, reserved=0)
+            n = lib().compresskv_cache_attend_workspace_bytes(self._ref, ctypes.byref(a))
+            if n == 0:   # the call itself says why
+                _check("compresskv_cache_attend", lib().compresskv_cache_attend(
+                    self._ref, ctypes.byref(a), _ptr(q), _ptr(q), 0, 0, 0))
+            known = self._attends[key] = (a, ctypes.byref(a), n)
+        ctx, handle = _enter(self.device, stream)
+        with ctx:
+            if out is None:
+                out = torch.empty_like(q)
+            if ws is None:
+                ws = torch.empty(known[2], dtype=torch.uint8, device=self.device)
+            _check("compresskv_cache_attend", lib().compresskv_cache_attend(
+                self._ref, known[1], q.data_ptr(), out.data_ptr(), ws.data_ptr(),
+                ws.numel() * ws.element_size(), handle))
+        return out
+
+    def evict(self, budget: int, *, n_sinks: int = 0, n_recent: int = 0, ws=None,
+              stream=None) -> None:
+        """Drops the slots of least weight of every group with more than `budget`."""
+        n = self._evict_bytes.get(budget)
+        if n is None:
+            n = lib().compresskv_cache_evict_workspace_bytes(self._ref, int(budget))
+            if n == 0:
+                raise CompressKVError("compresskv_cache_evict", INVALID_ARGUMENT)
+            self._evict_bytes[budget] = n
+        ctx, handle = _enter(self.device, stream)
+        with ctx:
+            if ws is None:
+                ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+            _check("compresskv_cache_evict", lib().compresskv_cache_evict(
+                self._ref, int(budget), int(n_sinks), int(n_recent), ws.data_ptr(),
+                ws.numel() * ws.element_size(), handle))
+
+
+class WindowProblem:
+    """A ckv_window_problem for one batch of sequences (its layers share it):
+    q [Tq, Hq, D], k, v [Tk, Hkv, D] with D contiguous and any strides; cu_q, cu_k
+    int32 [batch + 1] on the device (host copies taken once here, unless given).
+    """
+
+    def __init__(self, q, k, v, cu_q, cu_k, *, window: int, n_sinks: int = 0,
+                 scale: float | None = None, cu_q_host=None, cu_k_host=None):
+        if q.dim() != 3 or k.dim() != 3 or v.shape != k.shape or q.shape[2] != k.shape[2]:
+            raise ValueError("q must be [Tq, Hq, D], k and v [Tk, Hkv, D]")
+        if q.dtype not in _DTYPES or k.dtype != q.dtype or v.dtype != q.dtype:
+            raise ValueError("q, k and v must share one dtype, bfloat16 or float32")
+        if q.stride(2) != 1 or k.stride(2) != 1 or v.stride(2) != 1:
+            raise ValueError("the head dimension of q, k and v must be contiguous")
+        self._host = []
+        for name, cu, host, rows in (("cu_q", cu_q, cu_q_host, q.shape[0]),
+                                     ("cu_k", cu_k, cu_k_host, k.shape[0])):
+            if cu.dtype != torch.int32 or cu.dim() != 1 or not cu.is_contiguous():
+                raise ValueError(f"{name} must be contiguous int32 [batch + 1]")
+            host = cu.cpu() if host is None else host
+            host = np.ascontiguousarray(host.numpy() if isinstance(host, torch.Tensor)
+                                        else np.asarray(host), dtype=np.int32)
+            if host.shape != tuple(cu.shape) or host.shape[0] < 2:
+                raise ValueError(f"{name} must have batch + 1 entries")
+            if int(host[-1]) > rows:
+                raise ValueError(f"{name} ends past the last row ({int(host[-1])} of {rows})")
+            self._host.append(host)
+        if cu_q.shape != cu_k.shape:
+            raise ValueError("cu_q and cu_k must have the same number of sequences")
+        for t in (k, v, cu_q, cu_k):
+            if t.device != q.device:
+                raise ValueError("q, k, v, cu_q and cu_k must be on one device")
+        self.cu_q, self.cu_k, self.device = cu_q, cu_k, q.device
+        self._layout = tuple((t.shape, t.stride(), t.dtype) for t in (q, k, v))
+        strides = {f"{n}_stride_{w}": t.stride(i) for n, t in (("q", q), ("k", k), ("v", v))
+                   for i, w in enumerate(("tok", "head"))}
+        self.c = CkvWindowProblem(
+            batch=cu_q.shape[0] - 1, n_q_heads=q.shape[1], n_kv_heads=k.shape[1],
+            head_dim=q.shape[2], dtype=_DTYPES[q.dtype], window=int(window), n_sinks=int(n_sinks),
+            scale=float(scale) if scale else 0.0, cu_q=_ptr(cu_q),
+            cu_q_host=self._host[0].ctypes.data, cu_k=_ptr(cu_k),
+            cu_k_host=self._host[1].ctypes.data, **strides)
+        self._ref = ctypes.byref(self.c)
+        self._ws_bytes = lib().compresskv_window_attention_workspace_bytes(self._ref)
+        if self._ws_bytes == 0:   # the call itself says why
+            _check("compresskv_window_attention", lib().compresskv_window_attention(
+                self._ref, 0, 0, 0, 0, 0, 0, 0))
+
+
+def window_attention(p: WindowProblem, q, k, v, *, out=None, ws=None, stream=None):
+    """Causal attention within p's window and first tokens: out [Tq, Hq, D].  q, k and v
+    are laid out as the tensors that p was made from."""
+    if tuple((t.shape, t.stride(), t.dtype) for t in (q, k, v)) != p._layout:
+        raise ValueError("q, k and v must have the shapes, strides and dtype of the problem")
+    for t in (q, k, v):
+        if t.device != p.device:
+            raise ValueError(f"q, k and v must be on {p.device}")
+    _check_on_gpu(p.device)
+    if out is not None:
+        _check_tensor(out, "out", q.shape, q.dtype, p.device)
+    ctx, handle = _enter(p.device, stream)
+    with ctx:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=p.device)
+        if ws is None:
+            ws = torch.empty(p._ws_bytes, dtype=torch.uint8, device=p.device)
+        _check("compresskv_window_attention", lib().compresskv_window_attention(
+            p._ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ws.data_ptr(),
+            ws.numel() * ws.element_size(), handle))
+    return out

@@ -1,0 +1,220 @@
+// Attention over a bounded cache (include/compresskv_cache.h): the entry point,
+// the join of split rows with the accumulation of the slots' weights, and the
+// dispatch of the attention kernel (attend_kernels.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "attend.h"
+#include "cache_api.h"
+#include "score_common.h"
+
+namespace ckv {
+
+// A row's reference and sum over its splits.
+__device__ __forceinline__ float2 join_row(const float2 *ml, int64_t stride, int splits) {
+  float top = -INFINITY;
+  for (int s = 0; s < splits; ++s) top = fmaxf(top, ml[s * stride].x);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  for (int s = 0; s < splits; ++s) sum += ml[s * stride].y * fast_exp2(ml[s * stride].x - ref);
+  return make_float2(ref, sum);
+}
+
+// Grid (out_blocks + weight blocks, groups), 256 threads.  The first out_blocks
+// join the splits' outputs (D / 4 lanes per row); each of the others adds to the
+// weights of 256 slots what the group's rows gave them, row by row in order.
+template <AttendSource SRC, typename T, int D>
+__global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, int out_blocks) {
+  const int tid = threadIdx.x, bg = blockIdx.y, RM = 16 * a.rt;
+  const int b = bg / a.Hkv, g = bg - b * a.Hkv;
+  const int64_t slot0 = (int64_t)bg * a.row_blocks * a.splits;
+  if ((int)blockIdx.x < out_blocks) {
+    const int q0 = SRC == kOverWindow ? a.cu_q[b] : 0;
+    const int rows = SRC == kOverWindow ? (a.cu_q[b + 1] - q0) * a.G : a.rows;
+    constexpr int LR = D / 4;                     // lanes per row
+    const int r = (int)blockIdx.x * (256 / LR) + tid / LR, d = 4 * (tid % LR);
+    if (r >= rows) return;
+    const int rb = r / RM, rr = r - rb * RM;
+    const float2 *ml = a.part_ml + (slot0 + (int64_t)rb * a.splits) * RM + rr;
+    const float2 all = join_row(ml, RM, a.splits);
+    const float *po = a.part_o + ((slot0 + (int64_t)rb * a.splits) * RM + rr) * D + d;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+      const float f = fast_exp2(ml[(int64_t)s * RM].x - all.x);
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(po + (int64_t)s * RM * D);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] += x[k] * f;
+    }
+    const float inv = all.y == 0.f ? 0.f : 1.f / all.y;
+    const int i = r / a.G, h = g * a.G + (r - i * a.G);
+    const int64_t token = SRC == kOverWindow ? (int64_t)q0 + i : (int64_t)b * a.n_q + i;
+    T *to = reinterpret_cast<T *>(a.out) + (token * ((int64_t)a.Hkv * a.G) + h) * D + d;
+    typedef T Tx4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<Tx4 *>(to) =
+        Tx4{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
+  } else if constexpr (SRC == kOverCache) {
+    __shared__ float2 row_s[64];                  // (reference, 1 / sum)
+    const int n = live_slots(a.c, bg);
+    const int s0 = ((int)blockIdx.x - out_blocks) * 256;
+    if (s0 >= n) return;                          // uniform
+    for (int r = tid; r < a.rows; r += 256) {
+      const int rb = r / RM, rr = r - rb * RM;
+      const float2 all = join_row(a.part_ml + (slot0 + (int64_t)rb * a.splits) * RM + rr, RM, a.splits);
+      row_s[r] = make_float2(all.x, all.y == 0.f ? 0.f : 1.f / all.y);
+    }
+    __syncthreads();
+    const int s = s0 + tid;
+    if (s >= n) return;
+    const float *z = a.logits + (int64_t)bg * a.rows * a.logit_stride + s;
+    float got = 0.f;
+    for (int r = 0; r < a.rows; ++r)
+      got += fast_exp2(__builtin_fmaf(z[r * a.logit_stride], a.c1, -row_s[r].x)) * row_s[r].y;
+    a.c.weight[(int64_t)bg * a.c.capacity + s] += got;
+  }
+}
+
+void launch_attend_join(const AttendArgs &a, AttendSource source, bool f32, int head_dim, int max_rows,
+                        hipStream_t stream) {
+  const int out_blocks = a.splits > 1 ? (max_rows + 256 / (head_dim / 4) - 1) / (256 / (head_dim / 4)) : 0;
+  const int weight_blocks = a.logits ? (a.c.capacity + 255) / 256 : 0;
+  if (out_blocks + weight_blocks == 0) return;
+  const dim3 grid(out_blocks + weight_blocks, a.c.groups);
+  auto go = [&]<AttendSource SRC, typename T, int D>() {
+    hipLaunchKernelGGL((attend_join_kernel<SRC, T, D>), grid, dim3(256), 0, stream, a, out_blocks);
+  };
+  auto dim = [&]<AttendSource SRC, typename T>() {
+    head_dim == 64 ? go.template operator()<SRC, T, 64>() : go.template operator()<SRC, T, 128>();
+  };
+  if (source == kOverCache)
+    f32 ? dim.template operator()<kOverCache, float>() : dim.template operator()<kOverCache, __bf16>();
+  else
+    f32 ? dim.template operator()<kOverWindow, float>() : dim.template operator()<kOverWindow, __bf16>();
+}
+
+// One per row type (attend_fp4.hip, attend_bf16.hip, attend_f32.hip).
+void launch_attend_fp4(const AttendArgs &a, bool f32, int head_dim, dim3 grid, hipStream_t stream);
+void launch_attend_bf16(const AttendArgs &a, AttendSource source, int head_dim, dim3 grid,
+                        hipStream_t stream);
+void launch_attend_f32(const AttendArgs &a, AttendSource source, int head_dim, dim3 grid,
+                       hipStream_t stream);
+
+void launch_attend(const AttendArgs &a, AttendSource source, CacheType type, bool f32, int head_dim,
+                   int max_rows, hipStream_t stream) {
+  const dim3 grid(a.row_blocks, a.c.groups, a.splits);
+  if (type == kCacheFp4) launch_attend_fp4(a, f32, head_dim, grid, stream);
+  else if (type == kCacheBf16) launch_attend_bf16(a, source, head_dim, grid, stream);
+  else launch_attend_f32(a, source, head_dim, grid, stream);
+  launch_attend_join(a, source, f32, head_dim, max_rows, stream);
+}
+
+// Row tiles per workgroup: one up to 16 rows, two up to 32, else four (two at
+// most for fp32 queries over 4-bit rows, whose three parts fill the registers).
+int attend_row_tiles(int rows, bool three_parts) {
+  return rows <= 16 ? 1 : rows <= 32 || three_parts ? 2 : 4;
+}
+
+// Workgroups a row block's keys are split over: about four per CU in all, each
+// with 128 keys (one step of every wave) at least.
+int attend_splits(int64_t blocks, int64_t keys) {
+  const int64_t most = std::max<int64_t>(1, (keys + 127) / 128);
+  return (int)std::min<int64_t>({std::max<int64_t>(1, 1024 / std::max<int64_t>(1, blocks)), most,
+                                 (int64_t)kAttendMaxSplits});
+}
+
+}  // namespace ckv
+
+using ckv_api::cache_view;
+using ckv_api::check_cache;
+using ckv_api::fail;
+using ckv_api::launched;
+using ckv_api::ok;
+using ckv_api::round_up;
+
+namespace {
+
+struct AttendPlan {
+  ckv::AttendArgs a;
+  size_t ml_bytes, o_bytes, logit_bytes;
+  size_t total() const { return ml_bytes + o_bytes + logit_bytes; }
+};
+
+int plan_attend(const ckv_cache *c, const ckv_attend_problem *p, AttendPlan &pl) {
+  int st;
+  if ((st = check_cache(c))) return st;
+  if (!p) return fail(CKV_INVALID_ARGUMENT, "attend problem is NULL");
+  if (p->reserved != 0) return fail(CKV_INVALID_ARGUMENT, "reserved must be 0");
+  if (p->accumulate != 0 && p->accumulate != 1)
+    return fail(CKV_INVALID_ARGUMENT, "accumulate must be 0 or 1 (got %d)", p->accumulate);
+  if (p->n_q < 1) return fail(CKV_INVALID_ARGUMENT, "n_q must be >= 1 (got %d)", p->n_q);
+  if (p->n_q_heads < 1 || p->n_q_heads % c->n_kv_heads)
+    return fail(CKV_INVALID_ARGUMENT, "n_q_heads must be a multiple of n_kv_heads (got %d, %d)",
+                p->n_q_heads, c->n_kv_heads);
+  if (!std::isfinite(p->scale)) return fail(CKV_INVALID_ARGUMENT, "scale must be finite");
+  if (p->dtype != CKV_F32 && p->dtype != CKV_BF16)
+    return fail(CKV_UNSUPPORTED, "queries must be CKV_F32 or CKV_BF16 (got %d)", p->dtype);
+  if (c->dtype != CKV_FP4 && p->dtype != c->dtype)
+    return fail(CKV_UNSUPPORTED, "queries over full rows must have the rows' dtype");
+  const int64_t rows = (int64_t)p->n_q * (p->n_q_heads / c->n_kv_heads);
+  if (rows > 64)
+    return fail(CKV_UNSUPPORTED, "n_q * n_q_heads / n_kv_heads must be <= 64 (got %lld)",
+                (long long)rows);
+  ckv::AttendArgs &a = pl.a;
+  a = ckv::AttendArgs{};
+  a.c = cache_view(c);
+  a.Hkv = c->n_kv_heads;
+  a.G = p->n_q_heads / c->n_kv_heads;
+  a.n_q = p->n_q;
+  a.rows = (int32_t)rows;
+  a.rt = ckv::attend_row_tiles(a.rows, c->dtype == CKV_FP4 && p->dtype == CKV_F32);
+  a.row_blocks = (a.rows + 16 * a.rt - 1) / (16 * a.rt);
+  a.splits = ckv::attend_splits((int64_t)a.c.groups * a.row_blocks, c->capacity);
+  a.logit_stride = round_up(c->capacity, 32);
+  const float scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)c->head_dim);
+  a.c1 = scale * 1.44269504088896340736f;
+  const size_t parts = (size_t)a.c.groups * a.row_blocks * a.splits * 16 * a.rt;
+  pl.ml_bytes = a.splits > 1 || p->accumulate ? round_up(parts * sizeof(float2), 256) : 0;
+  pl.o_bytes = a.splits > 1 ? round_up(parts * c->head_dim * sizeof(float), 256) : 0;
+  pl.logit_bytes =
+      p->accumulate ? round_up((size_t)a.c.groups * a.rows * a.logit_stride * sizeof(float), 256) : 0;
+  return CKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t compresskv_cache_attend_workspace_bytes(const ckv_cache *c, const ckv_attend_problem *p) {
+  AttendPlan pl;
+  if (plan_attend(c, p, pl)) return 0;
+  ok();
+  return std::max<size_t>(256, pl.total());
+}
+
+int compresskv_cache_attend(const ckv_cache *c, const ckv_attend_problem *p, const void *q,
+                            void *out, void *ws, size_t ws_bytes, void *stream) {
+  AttendPlan pl;
+  int st;
+  if ((st = plan_attend(c, p, pl))) return st;
+  if (!q || !out) return fail(CKV_INVALID_ARGUMENT, "q and out are required");
+  if (!ckv_api::aligned(q, 16) || !ckv_api::aligned(out, 16))
+    return fail(CKV_UNSUPPORTED, "q and out must be 16-byte aligned");
+  if (!ws) return fail(CKV_INVALID_ARGUMENT, "ws is NULL");
+  if (!ckv_api::aligned(ws, 256)) return fail(CKV_UNSUPPORTED, "ws must be 256-byte aligned");
+  if (ws_bytes < std::max<size_t>(256, pl.total()))
+    return fail(CKV_WORKSPACE_TOO_SMALL, "workspace of %zu bytes needed, %zu given",
+                std::max<size_t>(256, pl.total()), ws_bytes);
+  ckv::AttendArgs &a = pl.a;
+  a.q = static_cast<const char *>(q);
+  a.out = static_cast<char *>(out);
+  char *w = static_cast<char *>(ws);
+  a.part_ml = reinterpret_cast<float2 *>(w);
+  a.part_o = reinterpret_cast<float *>(w + pl.ml_bytes);
+  a.logits = p->accumulate ? reinterpret_cast<float *>(w + pl.ml_bytes + pl.o_bytes) : nullptr;
+  ckv::launch_attend(a, ckv::kOverCache, (ckv::CacheType)c->dtype, p->dtype == CKV_F32, c->head_dim,
+                     a.rows, (hipStream_t)stream);
+  return launched("cache attend");
+}
+
+}  // extern "C"

@@ -1,0 +1,129 @@
+"""Windowed attention with sinks on the GPU against the oracle."""
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache_oracle as CO
+from paper_2606_24467_amd import compresskv as C
+from tests import cache_helpers as H
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def _inputs(spans, hq, hkv, d, dtype, gpu, seed, layout="kv"):
+    """q, k, v of packed sequences with (queries, keys) each; K and V interleaved."""
+    g = torch.Generator(device=gpu).manual_seed(seed)
+    tq, tk = (sum(s[i] for s in spans) for i in (0, 1))
+    q = torch.randn((tq + 3, hq, d), generator=g, device=gpu).to(dtype)   # rows past the end
+    kv = torch.randn((tk + 2, 2, hkv, d), generator=g, device=gpu).to(dtype)
+    k, v = kv[:, 0], kv[:, 1]
+    if layout == "heads":     # [heads, tokens, D] seen as [tokens, heads, D]
+        q, k, v = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v))
+    k[tk:], v[tk:] = float("nan"), float("nan")
+    cu = [torch.tensor(np.cumsum([0] + [s[i] for s in spans]), dtype=torch.int32, device=gpu)
+          for i in (0, 1)]
+    return q, k, v, cu[0], cu[1]
+
+
+def _check(q, k, v, spans, window, sinks, out, scale=None, bits=8):
+    d, hq, hkv = q.shape[2], q.shape[1], k.shape[1]
+    c = 1.0 / np.sqrt(d) if scale is None else scale
+    q0 = k0 = 0
+    o, qv, kv, vv = (H.values(x) for x in (out, q, k, v))
+    for lq, lk in spans:
+        t = lk - lq + np.arange(lq)[:, None]
+        j = np.arange(lk)[None, :]
+        sees = (j <= t) & ((j > t - window) | (j < sinks))
+        want = CO.window_attention(qv[q0:q0 + lq], kv[k0:k0 + lk], vv[k0:k0 + lk], window, sinks, c)
+        for h in range(hq):
+            g = h // (hq // hkv)
+            kk, vg = kv[k0:k0 + lk, g], vv[k0:k0 + lk, g]
+            got, w = o[q0:q0 + lq, h], want[:, h]
+            assert (np.isnan(got) == np.isnan(w)).all()
+            with np.errstate(invalid="ignore"):
+                p = CO._softmax_rows(c * (qv[q0:q0 + lq, h] @ kk.T), sees)
+                dz = H.logit_error(qv[q0:q0 + lq, h], kk, c)
+                tol = H.attention_tolerance(w, p, sees, dz, vg, q.dtype, H.p_part(q.dtype, bits))
+            fine = np.isfinite(w)
+            assert (np.abs(got - w) <= tol)[fine].all(), (lq, lk, h, np.nanmax(np.abs(got - w) / tol))
+            assert (got[~fine & ~np.isnan(w)] == w[~fine & ~np.isnan(w)]).all()
+        q0, k0 = q0 + lq, k0 + lk
+
+
+CASES = [   # spans (queries, keys), Hq, Hkv, D, window, sinks
+    ([(1, 1), (1, 33), (1, 700)], 8, 2, 128, 64, 4),
+    ([(1, 5), (1, 2000)], 28, 4, 128, 1 << 30, 0),
+    ([(1, 900)], 16, 1, 64, 100, 130),
+    ([(3, 70), (16, 16), (2, 300)], 8, 2, 64, 50, 4),
+    ([(130, 130), (65, 200), (0, 40), (1, 1)], 8, 2, 128, 33, 4),
+    ([(257, 257)], 28, 4, 128, 1, 0),
+    ([(257, 300)], 28, 4, 128, 1, 2),
+    ([(128, 128), (64, 64)], 8, 8, 64, 16, 0),
+    ([(200, 200)], 16, 1, 128, 77, 100),
+    ([(300, 300)], 4, 2, 128, 4096, 0),
+    ([(40, 25), (5, 0), (20, 20)], 8, 2, 128, 7, 3),          # more queries than keys
+    ([(511, 1030)], 8, 2, 128, 256, 64),
+    ([(333, 333)], 6, 2, 64, 128, 16),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0][0]}x{len(c[0])}-{c[1]}-{c[2]}-{c[3]}-{c[4]}-{c[5]}")
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_window_attention(gpu, case, dtype):
+    spans, hq, hkv, d, window, sinks = case
+    print("window", case, dtype, file=sys.stderr, flush=True)
+    q, k, v, cu_q, cu_k = _inputs(spans, hq, hkv, d, dtype, gpu, 1)
+    p = C.WindowProblem(q, k, v, cu_q, cu_k, window=window, n_sinks=sinks)
+    out = torch.full_like(q, 7.0)
+    C.window_attention(p, q, k, v, out=out)
+    n = sum(s[0] for s in spans)
+    _check(q, k, v, spans, window, sinks, out)
+    assert (out[n:] == 7.0).all()                             # rows past the last sequence
+    again = C.window_attention(p, q, k, v)
+    assert (H.bits(again[:n]) == H.bits(out[:n])).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_window_attention_strides_and_scale(gpu, dtype):
+    spans = [(150, 150), (20, 90)]
+    q, k, v, cu_q, cu_k = _inputs(spans, 8, 2, 64, dtype, gpu, 2, layout="heads")
+    p = C.WindowProblem(q, k, v, cu_q, cu_k, window=40, n_sinks=4, scale=0.3)
+    _check(q, k, v, spans, 40, 4, C.window_attention(p, q, k, v), scale=0.3)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_keys_that_a_query_does_not_see_may_hold_anything(gpu, dtype):
+    """Infinities and NaN in K and V reach the queries that see them and no other."""
+    spans = [(300, 300), (1, 500)]
+    q, k, v, cu_q, cu_k = _inputs(spans, 8, 2, 128, dtype, gpu, 3)
+    for j, x in ((5, float("inf")), (100, float("nan")), (177, -float("inf")), (299, float("nan")),
+                 (310, float("inf")), (480, float("nan"))):
+        v[j, :, 17] = x
+    v[178, :, 17] = float("inf")
+    k[40] = float("nan")
+    k[400] = float("inf")
+    p = C.WindowProblem(q, k, v, cu_q, cu_k, window=16, n_sinks=4)
+    out = C.window_attention(p, q, k, v)
+    _check(q, k, v, spans, 16, 4, out)
+    assert torch.isfinite(out[300]).all()
+
+
+def test_a_long_sequence_in_pieces(gpu):
+    """Chunks of a prompt and single tokens give what the whole prompt gives."""
+    n, window = 1000, 200
+    q, k, v, cu, _ = _inputs([(n, n)], 8, 2, 128, BF16, gpu, 4)
+    p = C.WindowProblem(q, k, v, cu, cu, window=window, n_sinks=4)
+    whole = H.values(C.window_attention(p, q, k, v))
+    for a, e in ((0, 130), (130, 999), (999, 1000), (500, 501)):
+        qq, kk, vv = q[a:e], k[:e], v[:e]
+        cu_q = torch.tensor([0, e - a], dtype=torch.int32, device=gpu)
+        cu_k = torch.tensor([0, e], dtype=torch.int32, device=gpu)
+        p = C.WindowProblem(qq, kk, vv, cu_q, cu_k, window=window, n_sinks=4)
+        got = H.values(C.window_attention(p, qq, kk, vv))
+        # both are off by at most half a step of bf16 in the output and in each probability
+        size = np.abs(H.values(v[:n])).max()
+        assert np.abs(got - whole[a:e]).max() <= 4 * 2.0 ** -8 * size
