@@ -18,7 +18,7 @@ LIBNAME = "libcompresskv.so"
 SOURCES = ["api.hip", "score_kernels.hip", "score_layers.hip", "onepass_score.hip",
            "select_gather_kernels.hip", "offline.hip", "decode_error.hip", "cache.hip",
            "attend.hip", "attend_fp4.hip", "attend_bf16.hip", "attend_f32.hip",
-           "window_attention.hip"]
+           "window_attention.hip", "window_prompt.hip"]
 ARCH = "gfx950"
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++20", "-fPIC",

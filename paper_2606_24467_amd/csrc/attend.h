@@ -39,6 +39,15 @@ enum AttendSource : int { kOverCache = 0, kOverWindow = 1 };
 void launch_attend(const AttendArgs &a, AttendSource source, CacheType type, bool f32, int head_dim,
                    int max_rows, hipStream_t stream);
 
+// bf16 prompts and chunks (window_prompt.hip): kPromptRows rows per workgroup, a.rt
+// that many 16-row tiles.
+constexpr int kPromptRows = 128;
+void launch_window_prompt(const AttendArgs &a, int head_dim, int max_rows, hipStream_t stream);
+
+// Joins the splits' outputs, and adds to the weights if a.logits.
+void launch_attend_join(const AttendArgs &a, AttendSource source, bool f32, int head_dim,
+                        int max_rows, hipStream_t stream);
+
 // Row tiles per workgroup for that many rows, and workgroups to split `keys` keys
 // of each of `blocks` row blocks over.
 int attend_row_tiles(int rows, bool three_parts);

@@ -20,9 +20,19 @@ constexpr int32_t kMaxTokens = 1 << 30;
 struct WindowPlan {
   ckv::AttendArgs a;
   int64_t max_rows;             // query rows of one (sequence, group)
+  bool prompt;                  // the kernel for many rows
   size_t ml_bytes, o_bytes;
   size_t total() const { return ml_bytes + o_bytes; }
 };
+
+// bf16 calls with more rows per group than this take the kernel for many rows.
+constexpr int64_t kFewRows = 64;
+
+// Workgroups that a row block's keys are split over in the kernel for many
+// rows: as many as two per CU in all leave room for, four tiles each at least.
+int prompt_splits(int64_t blocks, int64_t keys) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / blocks, (keys + 255) / 256, 64}));
+}
 
 int check_cu(const int32_t *cu, int batch, const char *name) {
   if (cu[0] != 0) return fail(CKV_INVALID_ARGUMENT, "%s[0] must be 0", name);
@@ -77,14 +87,17 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
     const int64_t lk = p->cu_k_host[b + 1] - p->cu_k_host[b];
     if (lq == 0) continue;
     pl.max_rows = std::max(pl.max_rows, lq * a.G);
-    const int64_t span = std::min<int64_t>(lq, 64 / a.G + 1);   // tokens of 64 rows
+    const int64_t span = std::min<int64_t>(lq, ckv::kPromptRows / a.G + 1);   // tokens of a block
     keys = std::max(keys, std::min<int64_t>(lk, (int64_t)p->window + p->n_sinks + span - 1));
   }
   if (pl.max_rows > INT32_MAX)
     return fail(CKV_UNSUPPORTED, "a sequence has 2^31 or more query rows per group");
-  a.rt = ckv::attend_row_tiles((int)pl.max_rows, false);
+  pl.prompt = p->dtype == CKV_BF16 && pl.max_rows > kFewRows;
+  a.rt = pl.prompt ? ckv::kPromptRows / 16 : ckv::attend_row_tiles((int)pl.max_rows, false);
   a.row_blocks = (int32_t)((pl.max_rows + 16 * a.rt - 1) / (16 * a.rt));
-  a.splits = ckv::attend_splits((int64_t)a.c.groups * a.row_blocks, keys);
+  const int64_t blocks = (int64_t)a.c.groups * a.row_blocks;
+  if (blocks > 1 << 23) return fail(CKV_UNSUPPORTED, "too many query rows for one launch");
+  a.splits = pl.prompt ? prompt_splits(blocks, keys) : ckv::attend_splits(blocks, keys);
   a.window = std::min(p->window, kMaxTokens);   // positions plus or minus either stay in 32 bits
   a.sinks = std::min(p->n_sinks, kMaxTokens);
   a.q_tok = p->q_stride_tok * size, a.q_head = p->q_stride_head * size;
@@ -139,8 +152,11 @@ int compresskv_window_attention(const ckv_window_problem *p, const void *q, cons
   a.part_ml = static_cast<float2 *>(ws);
   a.part_o = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.ml_bytes);
   const bool f32 = p->dtype == CKV_F32;
-  ckv::launch_attend(a, ckv::kOverWindow, f32 ? ckv::kCacheF32 : ckv::kCacheBf16, f32, p->head_dim,
-                     (int)pl.max_rows, (hipStream_t)stream);
+  if (pl.prompt)
+    ckv::launch_window_prompt(a, p->head_dim, (int)pl.max_rows, (hipStream_t)stream);
+  else
+    ckv::launch_attend(a, ckv::kOverWindow, f32 ? ckv::kCacheF32 : ckv::kCacheBf16, f32, p->head_dim,
+                       (int)pl.max_rows, (hipStream_t)stream);
   return launched("window attention");
 }
 
