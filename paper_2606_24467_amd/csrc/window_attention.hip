@@ -92,7 +92,8 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
   }
   if (pl.max_rows > INT32_MAX)
     return fail(CKV_UNSUPPORTED, "a sequence has 2^31 or more query rows per group");
-  pl.prompt = p->dtype == CKV_BF16 && pl.max_rows > kFewRows;
+  pl.prompt = p->dtype == CKV_BF16 && pl.max_rows > kFewRows &&
+              std::max(p->k_stride_tok, p->v_stride_tok) * size <= ckv::kPromptMaxStride;
   a.rt = pl.prompt ? ckv::kPromptRows / 16 : ckv::attend_row_tiles((int)pl.max_rows, false);
   a.row_blocks = (int32_t)((pl.max_rows + 16 * a.rt - 1) / (16 * a.rt));
   const int64_t blocks = (int64_t)a.c.groups * a.row_blocks;

@@ -27,7 +27,6 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kPromptWaves = 4;
 static_assert(kPromptRows == 32 * kPromptWaves, "32 rows per wave");
-constexpr int64_t kNearStride = 1 << 24;         // bytes: 64 rows stay within 32 bits
 constexpr int kPromptKeys = 64;                  // keys per tile
 
 // The 32-row form of add_unbounded (attend_kernels.h), with the values of V that
@@ -56,7 +55,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   constexpr int U = D / 8;                       // 16-byte units per row
   constexpr int LD = kPromptKeys * U / (64 * kPromptWaves);   // loads of K (of V) per wave and tile
   constexpr int RB = D * 2;                      // bytes of a row in LDS
-  __shared__ __align__(16) char kv_s[2][2][kPromptKeys * RB];   // [buffer][K, V]
+  // Two buffers, each K then V.  They are two arrays, which the loop's two copies
+  // name: the compiler then sees that reads of one need not wait for the loads that
+  // are under way to the other.
+  constexpr int KB = kPromptKeys * RB;
+  __shared__ __align__(16) char even_s[2 * KB], odd_s[2 * KB];
+  static_assert(kPromptRows / 2 * (D + 8) * 2 <= 2 * KB, "half of the outputs fits a buffer");
   __shared__ int wild_s[2][kPromptWaves];        // a wave's loads held V values that are not finite
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -105,65 +109,68 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   // each) fall on banks of their own.
   auto swizzle_k = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
   auto swizzle_v = [](int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; };
-  const char *kg = a.k + k0 * a.k_tok + g * a.k_head, *vg = a.v + k0 * a.v_tok + g * a.v_head;
-  // Behind the sinks a tile is a run of rows: a base that every lane shares, and
-  // offsets in 32 bits that stay, where the strides are short enough for that.
-  const bool near = a.k_tok <= kNearStride && a.v_tok <= kNearStride;
+  // A tile is a run of rows: a base that every lane shares and offsets in 32 bits
+  // (the host sends longer strides elsewhere), but for the tile that the sinks end
+  // in and the last one, whose keys past the end read the last one.
+  const int k_row = (int)a.k_tok, v_row = (int)a.v_tok;
+  const char *kg = a.k + (k0 + shift) * a.k_tok + g * a.k_head;   // virtual key 0 behind the sinks
+  const char *vg = a.v + (k0 + shift) * a.v_tok + g * a.v_head;
   int k_off[LD], v_off[LD];
 #pragma unroll
   for (int i = 0; i < LD; ++i) {
     const int unit = 64 * (wave + kPromptWaves * i) + lane, row = unit / U, u = unit % U;
-    k_off[i] = near ? row * (int)a.k_tok + 16 * (u ^ swizzle_k(row)) : 0;
-    v_off[i] = near ? row * (int)a.v_tok + 16 * (u ^ swizzle_v(row)) : 0;
+    k_off[i] = row * k_row + 16 * (u ^ swizzle_k(row));
+    v_off[i] = row * v_row + 16 * (u ^ swizzle_v(row));
   }
   typedef __attribute__((address_space(3))) void *lds_ptr;
   typedef const __attribute__((address_space(1))) void *global_ptr;
-  auto load = [&](int tile, int buf) {
+  auto load = [&]<int BUF>(int tile) {
+    char *to = BUF ? odd_s : even_s;
     const int x0 = tile * kPromptKeys;
-    if (near && x0 >= sinks && x0 + kPromptKeys <= n) {      // uniform
-      const char *kt = kg + (int64_t)(x0 + shift) * a.k_tok, *vt = vg + (int64_t)(x0 + shift) * a.v_tok;
+    const char *kt = kg + (int64_t)x0 * k_row, *vt = vg + (int64_t)x0 * v_row;
+    if (x0 >= sinks && x0 + kPromptKeys <= n) {  // uniform
 #pragma unroll
       for (int i = 0; i < LD; ++i) {
         const int at = 64 * (wave + kPromptWaves * i) * 16;
-        __builtin_amdgcn_global_load_lds((global_ptr)(kt + (uint32_t)k_off[i]), (lds_ptr)&kv_s[buf][0][at], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((global_ptr)(vt + (uint32_t)v_off[i]), (lds_ptr)&kv_s[buf][1][at], 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_ptr)(kt + (uint32_t)k_off[i]), (lds_ptr)(to + at), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_ptr)(vt + (uint32_t)v_off[i]), (lds_ptr)(to + KB + at), 16, 0, 0);
       }
-    } else {                                     // keys past the end read the last one
+    } else {
 #pragma unroll
       for (int i = 0; i < LD; ++i) {
         const int at = 64 * (wave + kPromptWaves * i) * 16;
-        const int unit = 64 * (wave + kPromptWaves * i) + lane, row = unit / U, u = unit % U;
-        const int x = min(x0 + row, n - 1);
-        const int64_t key = x < sinks ? x : x + shift;
-        __builtin_amdgcn_global_load_lds((global_ptr)(kg + key * a.k_tok + 16 * (u ^ swizzle_k(row))),
-                                         (lds_ptr)&kv_s[buf][0][at], 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((global_ptr)(vg + key * a.v_tok + 16 * (u ^ swizzle_v(row))),
-                                         (lds_ptr)&kv_s[buf][1][at], 16, 0, 0);
+        const int row = (64 * (wave + kPromptWaves * i) + lane) / U, x = min(x0 + row, n - 1);
+        const int64_t back = x < sinks ? x - shift : x, over = x0 + row;   // its row, and the run's
+        __builtin_amdgcn_global_load_lds((global_ptr)(kt + (back - over) * k_row + k_off[i]),
+                                         (lds_ptr)(to + at), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((global_ptr)(vt + (back - over) * v_row + v_off[i]),
+                                         (lds_ptr)(to + KB + at), 16, 0, 0);
       }
     }
   };
-  // Whether rows at positions tf .. tl all see all of a tile.
-  auto all_seen = [&](int tile, int tf, int tl) {
-    const int x0 = tile * kPromptKeys, x1 = x0 + kPromptKeys - 1;
-    return x1 + shift <= tf && x1 < n &&
-           ((x0 >= sinks && x0 + shift > tl - a.window) || x1 < a.sinks || tl - a.window < 0);
+  // Virtual keys that every row of this wave, and of the workgroup, sees: a tile
+  // within them needs no mask.
+  const int w_from = max(sinks, wt_last - a.window - shift + 1), w_to = min(n - 1, wt_first - shift);
+  const int g_from = max(sinks, t_last - a.window - shift + 1), g_to = min(n - 1, t_first - shift);
+  auto within = [](int tile, int from, int to) {
+    return tile * kPromptKeys >= from && tile * kPromptKeys + kPromptKeys - 1 <= to;
   };
   // Waits for this wave's loads of a tile; where some row sees a part of it only,
   // looks for V values that are not finite among them.
-  auto arrive = [&](int tile, int buf) {
+  auto arrive = [&]<int BUF>(int tile) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (all_seen(tile, t_first, t_last)) return;
+    if (within(tile, g_from, g_to)) return;
     uint32_t wild = 0;                           // a carry out of an exponent of all ones
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
       const uint4 x = *reinterpret_cast<const uint4 *>(
-          &kv_s[buf][1][(64 * (wave + kPromptWaves * i) + lane) * 16]);
+          (BUF ? odd_s : even_s) + KB + (64 * (wave + kPromptWaves * i) + lane) * 16);
       const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) wild |= ((w[e] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
     }
     const bool any = __any(wild != 0);
-    if (lane == 0) wild_s[buf][wave] = any;
+    if (lane == 0) wild_s[BUF][wave] = any;
   };
   // this lane's places in a tile: of K fragment f in row c, of V block d in row
   // 4 h + (lane & 15) / 4 (rows 8 and 16 further on are swizzled alike)
@@ -178,114 +185,149 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   }
 
   f32x16 acc[DB];
-  float m, l;
+#pragma unroll
+  for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
+  float m = -INFINITY, l = 0.f;
 
-  // All tiles of this workgroup.  UNBOUNDED: with care for V values that are not
-  // finite, in keys that some rows do not see; the other form stops when it meets
-  // such a key (every wave at the same tile) and returns true.
-  auto walk = [&]<bool UNBOUNDED>() {
+  // the virtual keys that this lane's row sees: first_x .. last_x and those before a.sinks
+  const int last_x = min(t - shift, n - 1) - 4 * h, first_x = t - shift - a.window + 1 - 4 * h;
+
+  // One tile.  UNBOUNDED: with care for V values that are not finite.
+  auto work = [&]<bool UNBOUNDED, int BUF>(int tile) {
+    const char *kt = BUF ? odd_s : even_s, *vt = kt + KB;
+    f32x16 s[2] = {f32x16{}, f32x16{}};
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+        s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            *reinterpret_cast<const bf16x8 *>(kt + k_at[f] + 32 * k * RB), q[f], s[k], 0, 0, 0);
+    if constexpr (!UNBOUNDED) {                  // half 0's fragments, then each product with one of half 1
+      __builtin_amdgcn_sched_group_barrier(0x100, NF, 0);
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, NF, 0);
+    }
+    if (UNBOUNDED || !within(tile, w_from, w_to)) {
+      const int from = tile * kPromptKeys, last = last_x - from, first = first_x - from;
+      const int sink = min(a.sinks - 4 * h - from, last + 1);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int x = 32 * k + 8 * (i >> 2) + (i & 3);
+          s[k][i] = (x >= first && x <= last) || x < sink ? s[k][i] : -INFINITY;
+        }
+    }
+    // (the maximum that returns a NaN needs no quieting of its operands)
+    float top = __builtin_elementwise_maximum(s[0][0], s[1][0]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i)
+      top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(s[0][i], s[1][i]), top);
+    top *= a.c1;
+    if (__any(top > m + 8.f)) {                  // the reference follows in steps of 2^8
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+      const float next = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
+      const float shrink = m == next ? 1.f : fast_exp2(m - next);
+      l *= shrink;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= shrink;
+      m = next;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      bf16x8 p[2], sees[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if constexpr (UNBOUNDED) sees[i >> 3][i & 7] = (__bf16)(s[k][i] != -INFINITY ? 1.f : 0.f);
+        const float x = fast_exp2(__builtin_fmaf(s[k][i], a.c1, -ref));
+        l += x;
+        p[i >> 3][i & 7] = (__bf16)x;
+      }
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          // 16 lanes read four rows, 16 head dimensions of each; lane i gets column i
+          typedef __attribute__((address_space(3))) i16x4 *lptr;
+          const char *at = vt + v_at[d] + (32 * k + 16 * half) * RB;
+          const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)at);
+          const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(at + 8 * RB));
+          bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+          if constexpr (UNBOUNDED) add_unbounded32(acc[d], vf, sees[half]);
+          acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[half], acc[d], 0, 0, 0);
+        }
+    }
+    if constexpr (!UNBOUNDED) {
+      // fragments of V four products ahead; the softmax of half 1 between the
+      // products of half 0
+      __builtin_amdgcn_sched_group_barrier(0x100, 8, 1);
+      __builtin_amdgcn_sched_group_barrier(0x402, 60, 1);
+#pragma unroll
+      for (int e = 0; e < 2 * DB; ++e) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+        __builtin_amdgcn_sched_group_barrier(0x402, 56 / (2 * DB), 1);
+      }
+#pragma unroll
+      for (int e = 0; e < 2 * DB; ++e) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+      }
+    }
+  };
+
+  // One step of the loop: the next tile's loads, this tile's work, the wait for the
+  // loads.  False: the tile has such values in keys that some row does not see.
+  auto step = [&]<int BUF>(int tile) {
+    if (!within(tile, g_from, g_to)) {           // uniform over the workgroup
+      int any = 0;
+#pragma unroll
+      for (int w = 0; w < kPromptWaves; ++w) any |= wild_s[BUF][w];
+      if (__any(any != 0)) return false;
+    }
+    if (tile + 1 < tile1) load.template operator()<1 - BUF>(tile + 1);
+    work.template operator()<false, BUF>(tile);
+    if (tile + 1 < tile1) arrive.template operator()<1 - BUF>(tile + 1);
+    __syncthreads();
+    return true;
+  };
+
+  bool wild = false;
+  if (tile0 < tile1) {
+    load.template operator()<0>(tile0);
+    arrive.template operator()<0>(tile0);
+  }
+  __syncthreads();
+  for (int tile = tile0; tile < tile1; tile += 2) {
+    if (!step.template operator()<0>(tile) ||
+        (tile + 1 < tile1 && !step.template operator()<1>(tile + 1))) {
+      wild = true;
+      break;
+    }
+  }
+  if (wild) {
+    // Some rows see a part only of a tile with V values that are not finite: all of
+    // it again, with care for them, one tile after the other.
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = f32x16{};
     m = -INFINITY;
     l = 0.f;
-    if (tile0 < tile1) {
-      load(tile0, 0);
-      arrive(tile0, 0);
-    }
-    __syncthreads();
     for (int tile = tile0; tile < tile1; ++tile) {
-      const int buf = (tile - tile0) & 1;
-      if constexpr (!UNBOUNDED) {
-        if (!all_seen(tile, t_first, t_last)) {  // uniform over the workgroup
-          int wild = 0;
-#pragma unroll
-          for (int w = 0; w < kPromptWaves; ++w) wild |= wild_s[buf][w];
-          if (__any(wild != 0)) return true;
-        }
-      }
-      if (tile + 1 < tile1) load(tile + 1, buf ^ 1);
-      const int x0 = tile * kPromptKeys, x1 = min(n, x0 + kPromptKeys) - 1;
-      // no row of this wave sees a key of the tile
-      const bool none = (x0 < sinks ? x0 : x0 + shift) > wt_last ||
-                        (x0 >= sinks && x0 + shift >= a.sinks && x1 + shift <= wt_first - a.window);
-      if (!none) {
-        const char *kt = &kv_s[buf][0][0], *vt = &kv_s[buf][1][0];
-        f32x16 s[2] = {f32x16{}, f32x16{}};
-#pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-            s[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                *reinterpret_cast<const bf16x8 *>(kt + k_at[f] + 32 * k * RB), q[f], s[k], 0, 0, 0);
-        if (UNBOUNDED || !all_seen(tile, wt_first, wt_last)) {
-          // the row sees the virtual keys x <= t - shift that are in its window
-          // (x > t - shift - window) or among the first a.sinks; the elements are
-          // counted from the tile's first key and this lane's half
-          const int from = x0 + 4 * h;
-          const int last = min(t - shift, n - 1) - from, first = t - shift - a.window + 1 - from;
-          const int sink = min(a.sinks - from, last + 1);
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int x = 32 * k + 8 * (i >> 2) + (i & 3);
-              s[k][i] = (x >= first && x <= last) || x < sink ? s[k][i] : -INFINITY;
-            }
-        }
-        // (the maximum that returns a NaN needs no quieting of its operands)
-        float top = __builtin_elementwise_maximum(s[0][0], s[1][0]);
-#pragma unroll
-        for (int i = 1; i < 16; ++i)
-          top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(s[0][i], s[1][i]), top);
-        top *= a.c1;
-        if (__any(top > m + 8.f)) {              // the reference follows in steps of 2^8
-          const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top),
-                                                           false, false);
-          const float next = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])));
-          const float shrink = m == next ? 1.f : fast_exp2(m - next);
-          l *= shrink;
-#pragma unroll
-          for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[d][i] *= shrink;
-          m = next;
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          bf16x8 p[2], sees[2];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            if constexpr (UNBOUNDED) sees[i >> 3][i & 7] = (__bf16)(s[k][i] != -INFINITY ? 1.f : 0.f);
-            const float x = fast_exp2(__builtin_fmaf(s[k][i], a.c1, -ref));
-            l += x;
-            p[i >> 3][i & 7] = (__bf16)x;
-          }
-#pragma unroll
-          for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-              // 16 lanes read four rows, 16 head dimensions of each; lane i gets column i
-              typedef __attribute__((address_space(3))) i16x4 *lptr;
-              const char *at = vt + v_at[d] + (32 * k + 16 * half) * RB;
-              const i16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)at);
-              const i16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(at + 8 * RB));
-              bf16x8 vf = __builtin_bit_cast(
-                  bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-              if constexpr (UNBOUNDED) add_unbounded32(acc[d], vf, sees[half]);
-              acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[half], acc[d], 0, 0, 0);
-            }
-        }
-      }
-      if (tile + 1 < tile1) arrive(tile + 1, buf ^ 1);
       __syncthreads();
+      load.template operator()<0>(tile);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      work.template operator()<true, 0>(tile);
     }
-    return false;
-  };
-  if (walk.template operator()<false>()) {
-    __syncthreads();                             // the flags have been read
-    walk.template operator()<true>();
   }
+  __syncthreads();                               // the buffers are done with
 
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
@@ -306,8 +348,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   const float inv = l == 0.f ? 0.f : 1.f / l;
   // each wave's 32 rows through LDS, so that whole rows go out in 16-byte lanes
   constexpr int OS = D + 8;
-  static_assert(kPromptRows * OS * 2 <= sizeof(kv_s), "the outputs fit the buffers");
-  __bf16(*o_s)[OS] = reinterpret_cast<__bf16(*)[OS]>(&kv_s[0][0][0]) + 32 * wave;
+  __bf16(*o_s)[OS] = reinterpret_cast<__bf16(*)[OS]>(wave < kPromptWaves / 2 ? even_s : odd_s) +
+                     32 * (wave % (kPromptWaves / 2));
 #pragma unroll
   for (int d = 0; d < DB; ++d)
 #pragma unroll
