@@ -20,12 +20,16 @@ struct AttendArgs {
   const int32_t *cu_q, *cu_k;         // window
   float2 *part_ml;                    // [groups][row_blocks][splits][16 RT] (reference, sum)
   float *part_o;                      // [groups][row_blocks][splits][16 RT][D]
-  float *logits;                      // accumulate: [groups][rows][logit_stride] raw q . k
+  float *logits;                      // accumulate (several splits): [groups][rows][logit_stride]
+                                      // raw q . k
   int64_t logit_stride;
   int32_t Hkv, G, n_q;                // n_q: cache only
   int32_t rows;                       // cache: n_q * G
   int32_t rt;                         // row tiles per workgroup: 1, 2 or 4
   int32_t row_blocks, splits;
+  int32_t accumulate;                 // cache: add to the weights
+  int32_t masks;                      // rows of a workgroup may see different keys
+  int32_t one;                        // one workgroup per row block, no join (16 rows at most)
   int32_t window, sinks;              // window
   float c1;                           // softmax scale * log2(e)
 };
@@ -34,7 +38,7 @@ struct AttendArgs {
 enum AttendSource : int { kOverCache = 0, kOverWindow = 1 };
 
 // Enqueues the attention (and the join of its splits, with the accumulation of
-// the weights if a.logits).  type: of the rows; f32: of q and out; max_rows: of
+// the weights if a.accumulate).  type: of the rows; f32: of q and out; max_rows: of
 // the group with the most.  a.c.groups and a.Hkv are read for either source.
 void launch_attend(const AttendArgs &a, AttendSource source, CacheType type, bool f32, int head_dim,
                    int max_rows, hipStream_t stream);
@@ -45,13 +49,14 @@ constexpr int kPromptRows = 128;
 constexpr int64_t kPromptMaxStride = 1 << 24;   // bytes between tokens: 64 rows stay within 32 bits
 void launch_window_prompt(const AttendArgs &a, int head_dim, int max_rows, hipStream_t stream);
 
-// Joins the splits' outputs, and adds to the weights if a.logits.
+// Joins the splits' outputs, and adds to the weights if a.accumulate.
 void launch_attend_join(const AttendArgs &a, AttendSource source, bool f32, int head_dim,
                         int max_rows, hipStream_t stream);
 
 // Row tiles per workgroup for that many rows, and workgroups to split `keys` keys
 // of each of `blocks` row blocks over.
 int attend_row_tiles(int rows, bool three_parts);
+bool attend_in_one(int64_t rows, int64_t keys, bool weights);
 int attend_splits(int64_t blocks, int64_t keys);
 
 }  // namespace ckv

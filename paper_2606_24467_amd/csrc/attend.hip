@@ -12,73 +12,109 @@
 
 namespace ckv {
 
-// A row's reference and sum over its splits.
-__device__ __forceinline__ float2 join_row(const float2 *ml, int64_t stride, int splits) {
+// A row's reference and 1 / sum (0: it saw nothing) over its splits, by one wave: a lane
+// per split, then butterflies.
+__device__ __forceinline__ float2 join_row(const float2 *ml, int64_t stride, int splits, int lane) {
+  float2 x[kAttendMaxSplits / 64];
   float top = -INFINITY;
-  for (int s = 0; s < splits; ++s) top = fmaxf(top, ml[s * stride].x);
+#pragma unroll
+  for (int i = 0; i < kAttendMaxSplits / 64; ++i) {
+    const int s = lane + 64 * i;
+    x[i] = s < splits ? ml[s * stride] : make_float2(-INFINITY, 0.f);
+    top = fmaxf(top, x[i].x);
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   const float ref = top == -INFINITY ? 0.f : top;
   float sum = 0.f;
-  for (int s = 0; s < splits; ++s) sum += ml[s * stride].y * fast_exp2(ml[s * stride].x - ref);
-  return make_float2(ref, sum);
+#pragma unroll
+  for (int i = 0; i < kAttendMaxSplits / 64; ++i) sum += x[i].y * fast_exp2(x[i].x - ref);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+  return make_float2(ref, sum == 0.f ? 0.f : 1.f / sum);
 }
 
+constexpr int64_t kOneKeys = 2048;
+constexpr int kJoinSlots = 1024;   // slots whose weights one workgroup adds to
+
 // Grid (out_blocks + weight blocks, groups), 256 threads.  The first out_blocks
-// join the splits' outputs (D / 4 lanes per row); each of the others adds to the
-// weights of 256 slots what the group's rows gave them, row by row in order.
+// join the splits' outputs, a row each: the splits are dealt to 1024 / D groups of
+// D / 4 lanes, whose sums are added in order.  Each of the others adds to the
+// weights of kJoinSlots slots what the group's rows gave them, row by row in
+// order.  Bound by the latency of its few dependent loads.
 template <AttendSource SRC, typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, int out_blocks) {
-  const int tid = threadIdx.x, bg = blockIdx.y, RM = 16 * a.rt;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bg = blockIdx.y, RM = 16 * a.rt;
   const int b = bg / a.Hkv, g = bg - b * a.Hkv;
   const int64_t slot0 = (int64_t)bg * a.row_blocks * a.splits;
   if ((int)blockIdx.x < out_blocks) {
+    constexpr int LR = D / 4, NP = 256 / LR;      // lanes per row, parts of the splits
+    __shared__ __align__(16) f32x4 part_s[NP][LR];
     const int q0 = SRC == kOverWindow ? a.cu_q[b] : 0;
     const int rows = SRC == kOverWindow ? (a.cu_q[b + 1] - q0) * a.G : a.rows;
-    constexpr int LR = D / 4;                     // lanes per row
-    const int r = (int)blockIdx.x * (256 / LR) + tid / LR, d = 4 * (tid % LR);
-    if (r >= rows) return;
-    const int rb = r / RM, rr = r - rb * RM;
+    const int r = blockIdx.x;
+    if (r >= rows) return;                        // uniform
+    const int rb = r / RM, rr = r - rb * RM, d = 4 * (tid % LR), part = tid / LR;
     const float2 *ml = a.part_ml + (slot0 + (int64_t)rb * a.splits) * RM + rr;
-    const float2 all = join_row(ml, RM, a.splits);
+    const float2 all = join_row(ml, RM, a.splits, lane);
     const float *po = a.part_o + ((slot0 + (int64_t)rb * a.splits) * RM + rr) * D + d;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
+#pragma unroll 4
+    for (int s = part; s < a.splits; s += NP) {
       const float f = fast_exp2(ml[(int64_t)s * RM].x - all.x);
       const f32x4 x = *reinterpret_cast<const f32x4 *>(po + (int64_t)s * RM * D);
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] += x[k] * f;
     }
-    const float inv = all.y == 0.f ? 0.f : 1.f / all.y;
-    const int i = r / a.G, h = g * a.G + (r - i * a.G);
-    const int64_t token = SRC == kOverWindow ? (int64_t)q0 + i : (int64_t)b * a.n_q + i;
-    T *to = reinterpret_cast<T *>(a.out) + (token * ((int64_t)a.Hkv * a.G) + h) * D + d;
-    typedef T Tx4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<Tx4 *>(to) =
-        Tx4{(T)(o[0] * inv), (T)(o[1] * inv), (T)(o[2] * inv), (T)(o[3] * inv)};
+    part_s[part][tid % LR] = o;
+    __syncthreads();
+    if (part == 0) {
+      for (int p = 1; p < NP; ++p) {
+        const f32x4 x = part_s[p][tid % LR];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] += x[k];
+      }
+      const int i = r / a.G, h = g * a.G + (r - i * a.G);
+      const int64_t token = SRC == kOverWindow ? (int64_t)q0 + i : (int64_t)b * a.n_q + i;
+      T *to = reinterpret_cast<T *>(a.out) + (token * ((int64_t)a.Hkv * a.G) + h) * D + d;
+      typedef T Tx4 __attribute__((ext_vector_type(4)));
+      *reinterpret_cast<Tx4 *>(to) = Tx4{(T)(o[0] * all.y), (T)(o[1] * all.y), (T)(o[2] * all.y),
+                                         (T)(o[3] * all.y)};
+    }
   } else if constexpr (SRC == kOverCache) {
     __shared__ float2 row_s[64];                  // (reference, 1 / sum)
     const int n = live_slots(a.c, bg);
-    const int s0 = ((int)blockIdx.x - out_blocks) * 256;
+    const int s0 = ((int)blockIdx.x - out_blocks) * kJoinSlots;
     if (s0 >= n) return;                          // uniform
-    for (int r = tid; r < a.rows; r += 256) {
+    for (int r = wave; r < a.rows; r += 4) {
       const int rb = r / RM, rr = r - rb * RM;
-      const float2 all = join_row(a.part_ml + (slot0 + (int64_t)rb * a.splits) * RM + rr, RM, a.splits);
-      row_s[r] = make_float2(all.x, all.y == 0.f ? 0.f : 1.f / all.y);
+      const float2 all = join_row(a.part_ml + (slot0 + (int64_t)rb * a.splits) * RM + rr, RM, a.splits, lane);
+      if (lane == 0) row_s[r] = all;
     }
     __syncthreads();
-    const int s = s0 + tid;
-    if (s >= n) return;
-    const float *z = a.logits + (int64_t)bg * a.rows * a.logit_stride + s;
-    float got = 0.f;
-    for (int r = 0; r < a.rows; ++r)
-      got += fast_exp2(__builtin_fmaf(z[r * a.logit_stride], a.c1, -row_s[r].x)) * row_s[r].y;
-    a.c.weight[(int64_t)bg * a.c.capacity + s] += got;
+    float got[kJoinSlots / 256] = {};
+    const float *z = a.logits + (int64_t)bg * a.rows * a.logit_stride;
+#pragma unroll 2
+    for (int r = 0; r < a.rows; ++r) {
+      const float2 all = row_s[r];
+#pragma unroll
+      for (int i = 0; i < kJoinSlots / 256; ++i) {
+        const int s = min(s0 + tid + 256 * i, n - 1);
+        got[i] += fast_exp2(__builtin_fmaf(z[r * a.logit_stride + s], a.c1, -all.x)) * all.y;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kJoinSlots / 256; ++i) {
+      const int s = s0 + tid + 256 * i;
+      if (s < n) a.c.weight[(int64_t)bg * a.c.capacity + s] += got[i];
+    }
   }
 }
 
 void launch_attend_join(const AttendArgs &a, AttendSource source, bool f32, int head_dim, int max_rows,
                         hipStream_t stream) {
-  const int out_blocks = a.splits > 1 ? (max_rows + 256 / (head_dim / 4) - 1) / (256 / (head_dim / 4)) : 0;
-  const int weight_blocks = a.logits ? (a.c.capacity + 255) / 256 : 0;
+  const int out_blocks = a.splits > 1 ? max_rows : 0;
+  const int weight_blocks = a.accumulate && !a.one ? (a.c.capacity + kJoinSlots - 1) / kJoinSlots : 0;
   if (out_blocks + weight_blocks == 0) return;
   const dim3 grid(out_blocks + weight_blocks, a.c.groups);
   auto go = [&]<AttendSource SRC, typename T, int D>() {
@@ -115,11 +151,17 @@ int attend_row_tiles(int rows, bool three_parts) {
   return rows <= 16 ? 1 : rows <= 32 || three_parts ? 2 : 4;
 }
 
-// Workgroups a row block's keys are split over: about four per CU in all, each
-// with 128 keys (one step of every wave) at least.
+// Whether one workgroup takes all keys of a group's rows, in one launch, instead of
+// several and a join: up to kOneKeys keys, and with weights 32 KB of logits.
+bool attend_in_one(int64_t rows, int64_t keys, bool weights) {
+  return rows <= 16 && keys <= kOneKeys && (!weights || rows * ((keys + 31) / 32 * 32) <= 8192);
+}
+
+// Workgroups a row block's keys are split over: two per CU in all (as many as the
+// registers let run at once), each with 128 keys (one step of every wave) at least.
 int attend_splits(int64_t blocks, int64_t keys) {
   const int64_t most = std::max<int64_t>(1, (keys + 127) / 128);
-  return (int)std::min<int64_t>({std::max<int64_t>(1, 1024 / std::max<int64_t>(1, blocks)), most,
+  return (int)std::min<int64_t>({std::max<int64_t>(1, 512 / std::max<int64_t>(1, blocks)), most,
                                  (int64_t)kAttendMaxSplits});
 }
 
@@ -169,15 +211,19 @@ int plan_attend(const ckv_cache *c, const ckv_attend_problem *p, AttendPlan &pl)
   a.rows = (int32_t)rows;
   a.rt = ckv::attend_row_tiles(a.rows, c->dtype == CKV_FP4 && p->dtype == CKV_F32);
   a.row_blocks = (a.rows + 16 * a.rt - 1) / (16 * a.rt);
-  a.splits = ckv::attend_splits((int64_t)a.c.groups * a.row_blocks, c->capacity);
   a.logit_stride = round_up(c->capacity, 32);
+  a.accumulate = p->accumulate;
+  a.masks = p->n_q > 1;
+  a.one = ckv::attend_in_one(rows, c->capacity, true);   // the same bits with and without
+  a.splits = a.one ? 1 : ckv::attend_splits((int64_t)a.c.groups * a.row_blocks, c->capacity);
   const float scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)c->head_dim);
   a.c1 = scale * 1.44269504088896340736f;
   const size_t parts = (size_t)a.c.groups * a.row_blocks * a.splits * 16 * a.rt;
-  pl.ml_bytes = a.splits > 1 || p->accumulate ? round_up(parts * sizeof(float2), 256) : 0;
+  pl.ml_bytes = a.splits > 1 || (p->accumulate && !a.one) ? round_up(parts * sizeof(float2), 256) : 0;
   pl.o_bytes = a.splits > 1 ? round_up(parts * c->head_dim * sizeof(float), 256) : 0;
   pl.logit_bytes =
-      p->accumulate ? round_up((size_t)a.c.groups * a.rows * a.logit_stride * sizeof(float), 256) : 0;
+      p->accumulate && !a.one
+          ? round_up((size_t)a.c.groups * a.rows * a.logit_stride * sizeof(float), 256) : 0;
   return CKV_OK;
 }
 
@@ -211,7 +257,7 @@ int compresskv_cache_attend(const ckv_cache *c, const ckv_attend_problem *p, con
   char *w = static_cast<char *>(ws);
   a.part_ml = reinterpret_cast<float2 *>(w);
   a.part_o = reinterpret_cast<float *>(w + pl.ml_bytes);
-  a.logits = p->accumulate ? reinterpret_cast<float *>(w + pl.ml_bytes + pl.o_bytes) : nullptr;
+  a.logits = reinterpret_cast<float *>(w + pl.ml_bytes + pl.o_bytes);
   ckv::launch_attend(a, ckv::kOverCache, (ckv::CacheType)c->dtype, p->dtype == CKV_F32, c->head_dim,
                      a.rows, (hipStream_t)stream);
   return launched("cache attend");

@@ -84,14 +84,22 @@ struct AttendQ {
 };
 
 // QP: parts of a query (1: bf16 queries, or fp32 ones over fp32 rows; 3: fp32
-// queries over 4-bit rows).
-template <AttendSource SRC, CacheType CT, int D, int RT, int QP>
-__global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendArgs a) {
+// queries over 4-bit rows).  MASKS: rows of a workgroup may see different keys.
+// ONE: a workgroup of eight waves takes all keys of its rows and, over a cache,
+// adds to the weights itself, from logits held in LDS: one launch and no
+// workspace, for few keys.
+template <AttendSource SRC, CacheType CT, int D, int RT, int QP, bool MASKS, bool ONE>
+__global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kernel(const AttendArgs a) {
+  constexpr int NW = (ONE ? 2 : 1) * kAttendWaves, NTH = 64 * NW;
+  // steps whose rows are in registers or under way, as many as the registers hold
+  constexpr int DEPTH = (ONE && MASKS) || (CT == kCacheF32 && RT == 4) ? 1
+                        : CT == kCacheFp4 && QP == 1 ? 3 : 2;
   using S = AttendShape<CT, D>;
   constexpr bool F32Q = CT == kCacheF32 || QP == 3;
   constexpr int NT = S::NT, KS = S::KS, NK = S::NK, DL = S::DL, VW = S::VW;
   constexpr int PP = QP == 3 ? 3 : 2;           // parts of P
   constexpr int RM = 16 * RT;
+  extern __shared__ __align__(16) float logit_s[];  // ONE: [rows][logit_stride]
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, quad = lane >> 4;
@@ -101,12 +109,10 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
   // the rows of this workgroup and the keys that any of them sees
   int rows, n, t_first = 0, t_last = 0, lo = 0, sinks = 0;
   int q0 = 0, k0 = 0;
-  bool row_masks;                               // some key is seen by some rows only
   if constexpr (SRC == kOverCache) {
     rows = a.rows;
     n = live_slots(a.c, bg);
     t_first = (int)((uint32_t)a.c.seen[bg] - (uint32_t)a.n_q);   // position of query token 0
-    row_masks = a.n_q > 1;
   } else {
     q0 = a.cu_q[b];
     k0 = a.cu_k[b];
@@ -118,7 +124,6 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
     lo = max(0, t_first - a.window + 1);
     sinks = min(a.sinks, lo);                   // sinks outside the window come first
     n = t_last < 0 ? 0 : sinks + t_last - lo + 1;
-    row_masks = t_first != t_last;
   }
   // virtual key x in [0, n) -> its row
   auto key_of = [&](int x) {
@@ -252,7 +257,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
         }
       }
       if constexpr (SRC == kOverCache) {
-        if (row_masks) {
+        if constexpr (MASKS) {
           const int32_t *p = a.c.pos + (int64_t)bg * a.c.capacity;
           const int s = base + 16 * t + 4 * quad;
           w.pos[t] = make_int4(p[min(s, n - 1)], p[min(s + 1, n - 1)], p[min(s + 2, n - 1)],
@@ -312,9 +317,9 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
     // ---- masks (uniform: none in most steps)
     const bool tail = base + KS > n;
     bool partial = false;                          // some key is seen by some rows only
-    if constexpr (SRC == kOverCache) {
-      partial = row_masks;
-    } else if (row_masks) {
+    if constexpr (MASKS && SRC == kOverCache) {
+      partial = true;
+    } else if constexpr (MASKS) {
       const int j0 = key_of(base), j1 = key_of(min(base + KS, n) - 1);
       partial = !(j1 <= t_first && (j0 > t_last - a.window || j1 < a.sinks));
     }
@@ -326,7 +331,9 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
           const int x = base + 16 * t + 4 * quad + i;
           const bool live = x < n;
           int j;
-          if constexpr (SRC == kOverCache) {
+          if constexpr (!MASKS) {
+            j = 0;
+          } else if constexpr (SRC == kOverCache) {
             const int p4[4] = {w.pos[t].x, w.pos[t].y, w.pos[t].z, w.pos[t].w};
             j = p4[i];
           } else {
@@ -335,7 +342,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
             bool sees = live;
-            if (partial) {
+            if (MASKS && partial) {
               sees = sees && j <= t_row[rt];
               if constexpr (SRC == kOverWindow)
                 sees = sees && (j > t_row[rt] - a.window || j < a.sinks);
@@ -350,15 +357,18 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
         }
     }
     if constexpr (SRC == kOverCache) {
-      if (a.logits) {
+      if (a.accumulate) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
           const int r = rb * RM + 16 * rt + c;
           if (r < rows) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-              *reinterpret_cast<f32x4 *>(a.logits + ((int64_t)bg * rows + r) * a.logit_stride + base +
-                                         16 * t + 4 * quad) = s[rt][t];
+            for (int t = 0; t < NT; ++t) {
+              float *z;
+              if constexpr (ONE) z = logit_s + r * (int)a.logit_stride;
+              else z = a.logits + ((int64_t)bg * rows + r) * a.logit_stride;
+              *reinterpret_cast<f32x4 *>(z + base + 16 * t + 4 * quad) = s[rt][t];
+            }
           }
         }
       }
@@ -408,7 +418,7 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
 #pragma unroll
         for (int j = 0; j < DL; ++j) {
           float vv = __uint_as_float(w.v[0][i][j]);
-          if (partial && __any(!(fabsf(vv) < INFINITY))) {
+          if (MASKS && partial && __any(!(fabsf(vv) < INFINITY))) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
               const float sees = s[rt][0][i] != -INFINITY ? 1.f : 0.f;
@@ -452,47 +462,58 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
 #pragma unroll
           for (int x = 0; x < PP; ++x) pf[rt][x][e] = part[x];
         }
-      bool plain = true;
-      if (partial) {
-        bool finite = true;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-          for (int h = 0; h < DL / 2; ++h)
-            finite = finite && (u[e][h] & 0x7F80u) != 0x7F80u && (u[e][h] & 0x7F800000u) != 0x7F800000u;
-        plain = !__any(!finite);
-      }
-#pragma unroll
-      for (int j = 0; j < DL; ++j) {
+      // the j-th value of the eight rows
+      auto v_frag = [&](int j) {
         uint4 x;
         const uint32_t sel = j & 1 ? 0x07060302u : 0x05040100u;
         x.x = __builtin_amdgcn_perm(u[1][j / 2], u[0][j / 2], sel);
         x.y = __builtin_amdgcn_perm(u[3][j / 2], u[2][j / 2], sel);
         x.z = __builtin_amdgcn_perm(u[5][j / 2], u[4][j / 2], sel);
         x.w = __builtin_amdgcn_perm(u[7][j / 2], u[6][j / 2], sel);
-        bf16x8 vf = __builtin_bit_cast(bf16x8, x);
-        if (!plain) {
-          bf16x8 up, down, none;
+        return __builtin_bit_cast(bf16x8, x);
+      };
+      if (MASKS && partial) {
+        uint32_t wild = 0;                         // a carry out of an exponent of all ones
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float f = (float)vf[e];
-            up[e] = (__bf16)(f == INFINITY ? 1.f : 0.f);
-            down[e] = (__bf16)(f == -INFINITY ? 1.f : 0.f);
-            none[e] = (__bf16)(f != f ? 1.f : 0.f);
-            vf[e] = (__bf16)(fabsf(f) < INFINITY ? f : 0.f);
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int h = 0; h < DL / 2; ++h) wild |= ((u[e][h] & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+        if (__any(wild != 0)) {
+#pragma unroll
+          for (int j = 0; j < DL; ++j) {
+            const bf16x8 vf = v_frag(j);
+            bf16x8 up, down, none;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float f = (float)vf[e];
+              up[e] = (__bf16)(f == INFINITY ? 1.f : 0.f);
+              down[e] = (__bf16)(f == -INFINITY ? 1.f : 0.f);
+              none[e] = (__bf16)(f != f ? 1.f : 0.f);
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+              bf16x8 sees;
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                sees[e] = (__bf16)(s[rt][e >> 2][e & 3] != -INFINITY ? 1.f : 0.f);
+              const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+              add_unbounded(acc[rt][j], __builtin_amdgcn_mfma_f32_16x16x32_bf16(up, sees, zero, 0, 0, 0),
+                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(down, sees, zero, 0, 0, 0),
+                            __builtin_amdgcn_mfma_f32_16x16x32_bf16(none, sees, zero, 0, 0, 0));
+            }
           }
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) {
-            bf16x8 sees;
+          for (int e = 0; e < 8; ++e)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              sees[e] = (__bf16)(s[rt][e >> 2][e & 3] != -INFINITY ? 1.f : 0.f);
-            const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-            add_unbounded(acc[rt][j], __builtin_amdgcn_mfma_f32_16x16x32_bf16(up, sees, zero, 0, 0, 0),
-                          __builtin_amdgcn_mfma_f32_16x16x32_bf16(down, sees, zero, 0, 0, 0),
-                          __builtin_amdgcn_mfma_f32_16x16x32_bf16(none, sees, zero, 0, 0, 0));
-          }
+            for (int h = 0; h < DL / 2; ++h) {
+              if ((u[e][h] & 0x7F80u) == 0x7F80u) u[e][h] &= 0xFFFF0000u;
+              if ((u[e][h] & 0x7F800000u) == 0x7F800000u) u[e][h] &= 0xFFFFu;
+            }
         }
+      }
+#pragma unroll
+      for (int j = 0; j < DL; ++j) {
+        const bf16x8 vf = v_frag(j);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -502,64 +523,81 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
     }
   };
 
-  // ---- the wave's steps, the next one's loads in flight during each
+  // ---- the wave's steps: each one's registers are loaded again as soon as it is done
   {
-    AttendRaw<CT, D> cur, nxt;
-    if (st0 + wave < st1) load(st0 + wave, cur);
-    for (int st = st0 + wave; st < st1; st += kAttendWaves) {
-      if (st + kAttendWaves < st1) load(st + kAttendWaves, nxt);
-      compute(st, cur);
-      cur = nxt;
+    AttendRaw<CT, D> w[DEPTH];
+    int st = st0 + wave;
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i)
+      if (st + i * NW < st1) load(st + i * NW, w[i]);
+    while (st < st1) {
+      bool done = false;
+#pragma unroll
+      for (int i = 0; i < DEPTH; ++i) {
+        if (done) continue;
+        compute(st, w[i]);
+        if (st + DEPTH * NW < st1) load(st + DEPTH * NW, w[i]);
+        st += NW;
+        done = st >= st1;
+      }
     }
   }
 
-  // ---- join the waves, a row tile at a time
-  constexpr int OS = D + 4;                        // padded row
-  __shared__ __align__(16) float o_s[kAttendWaves][16][OS];
-  __shared__ float2 ml_s[kAttendWaves][RM];
+  // ---- join the waves: of every lane's output, four runs of DL head dimensions
+  constexpr int OS = 4 * DL + 4;                   // padded row of one run of the four quads
+  __shared__ __align__(16) float o_s[NW][16][OS];
+  __shared__ float2 ml_s[NW][RM];
+  __shared__ float2 row_s[RM];                     // (reference, 1 / sum) of the joined rows
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     l[rt] = quad_sum(l[rt]);
     if (quad == 0) ml_s[wave][16 * rt + c] = make_float2(m[rt], l[rt]);
   }
+  __syncthreads();
   const int64_t slot = ((int64_t)bg * a.row_blocks + rb) * a.splits + split;
+  if (tid < RM) {
+    float top = -INFINITY;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    if (rt) __syncthreads();
-    // lane: head dimensions 4 DL quad .. 4 DL quad + 4 DL - 1 of row c
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, ml_s[w][tid].x);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int w = 0; w < NW; ++w) {
+      const float f = fast_exp2(ml_s[w][tid].x - ref);
+      sum += ml_s[w][tid].y * f;
+      ml_s[w][tid].x = f;                          // the wave's share from here on
+    }
+    row_s[tid] = make_float2(ref, sum == 0.f ? 0.f : 1.f / sum);
+    if (!ONE && (a.splits > 1 || a.accumulate) && rb * RM + tid < rows)
+      a.part_ml[slot * RM + tid] = make_float2(top, sum);
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (rt || i) __syncthreads();
 #pragma unroll
       for (int j = 0; j < DL; j += 4)
-        *reinterpret_cast<f32x4 *>(&o_s[wave][c][DL * (4 * quad + i) + j]) =
+        *reinterpret_cast<f32x4 *>(&o_s[wave][c][DL * quad + j]) =
             f32x4{acc[rt][j][i], acc[rt][j + 1][i], acc[rt][j + 2][i], acc[rt][j + 3][i]};
-    __syncthreads();
-#pragma unroll
-    for (int it = 0; it < 16 * D / 4 / 256; ++it) {
-      const int e = tid + 256 * it, row = e / (D / 4), d = 4 * (e % (D / 4));
+      __syncthreads();
+      // 16 rows of 4 DL values, four to a thread: value DL quad + j is head dimension
+      // DL (4 quad + i) + j
+      const int row = tid / DL, x = 4 * (tid % DL), d = DL * (4 * (x / DL) + i) + x % DL;
       const int r = rb * RM + 16 * rt + row;
-      if (r < rows) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, ml_s[w][16 * rt + row].x);
-        const float ref = top == -INFINITY ? 0.f : top;
-        float sum = 0.f;
+      if (row < 16 && r < rows) {
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) {
-          const float2 ml = ml_s[w][16 * rt + row];
-          const float f = fast_exp2(ml.x - ref);
-          sum += ml.y * f;
-          const f32x4 x = *reinterpret_cast<const f32x4 *>(&o_s[w][row][d]);
+        for (int w = 0; w < NW; ++w) {
+          const float f = ml_s[w][16 * rt + row].x;
+          const f32x4 v = *reinterpret_cast<const f32x4 *>(&o_s[w][row][x]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[k] += x[k] * f;
+          for (int k = 0; k < 4; ++k) o[k] += v[k] * f;
         }
-        if ((a.splits > 1 || a.logits) && d == 0)
-          a.part_ml[slot * RM + 16 * rt + row] = make_float2(top, sum);
-        if (a.splits > 1) {
+        if (!ONE && a.splits > 1) {
           *reinterpret_cast<f32x4 *>(a.part_o + (slot * RM + 16 * rt + row) * D + d) = o;
         } else {
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          const float inv = row_s[16 * rt + row].y;
           char *to = const_cast<char *>(row_ptr(a.out, r, true)) + d * (F32Q ? 4 : 2);
           if constexpr (F32Q) {
             *reinterpret_cast<f32x4 *>(to) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
@@ -571,7 +609,23 @@ __global__ __launch_bounds__(64 * kAttendWaves) void attend_kernel(const AttendA
         }
       }
     }
+  if constexpr (ONE && SRC == kOverCache) {        // (one row block)
+    if (a.accumulate)
+      for (int x = tid; x < n; x += NTH) {
+        float got = 0.f;
+        for (int r = 0; r < rows; ++r)
+          got += fast_exp2(__builtin_fmaf(logit_s[r * (int)a.logit_stride + x], a.c1, -row_s[r].x)) *
+                 row_s[r].y;
+        a.c.weight[(int64_t)bg * a.c.capacity + x] += got;
+      }
   }
+}
+
+template <AttendSource SRC, CacheType CT, int D, int RT, int QP, bool MASKS, bool ONE>
+void launch_attend_as(const AttendArgs &a, dim3 grid, hipStream_t stream) {
+  const size_t lds = ONE && a.accumulate ? (size_t)a.rows * a.logit_stride * sizeof(float) : 0;
+  hipLaunchKernelGGL((attend_kernel<SRC, CT, D, RT, QP, MASKS, ONE>), grid,
+                     dim3(64 * (ONE ? 2 : 1) * kAttendWaves), lds, stream, a);
 }
 
 }  // namespace ckv

@@ -98,7 +98,11 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
   a.row_blocks = (int32_t)((pl.max_rows + 16 * a.rt - 1) / (16 * a.rt));
   const int64_t blocks = (int64_t)a.c.groups * a.row_blocks;
   if (blocks > 1 << 23) return fail(CKV_UNSUPPORTED, "too many query rows for one launch");
-  a.splits = pl.prompt ? prompt_splits(blocks, keys) : ckv::attend_splits(blocks, keys);
+  a.masks = pl.max_rows > a.G;   // more than one token in some row block
+  a.one = !pl.prompt && ckv::attend_in_one(pl.max_rows, keys, false);
+  a.splits = pl.prompt ? prompt_splits(blocks, keys)
+             : a.one   ? 1
+                       : ckv::attend_splits(blocks, keys);
   a.window = std::min(p->window, kMaxTokens);   // positions plus or minus either stay in 32 bits
   a.sinks = std::min(p->n_sinks, kMaxTokens);
   a.q_tok = p->q_stride_tok * size, a.q_head = p->q_stride_head * size;

@@ -184,7 +184,7 @@ def test_refused_calls_leave_everything(gpu):
     with pytest.raises(ValueError):
         cache.read(torch.float16)
     with pytest.raises(C.CompressKVError):
-        cache.attend(q, ws=torch.empty(1024, dtype=torch.uint8, device=gpu), accumulate=True)
+        cache.attend(q, ws=torch.empty(128, dtype=torch.uint8, device=gpu), accumulate=True)
     full = H.make_cache(C, torch.float32, [[3]], 8, 64, gpu, 1)
     with pytest.raises(C.CompressKVError):
         full.attend(torch.zeros(1, 1, 1, 64, dtype=torch.bfloat16, device=gpu))
