@@ -29,6 +29,7 @@ struct AttendArgs {
   int32_t row_blocks, splits;
   int32_t accumulate;                 // cache: add to the weights
   int32_t masks;                      // rows of a workgroup may see different keys
+  int32_t join_rows;                  // rows per workgroup of the join (set by its launcher)
   int32_t one;                        // one workgroup per row block, no join (16 rows at most)
   int32_t window, sinks;              // window
   float c1;                           // softmax scale * log2(e)
@@ -50,7 +51,7 @@ constexpr int64_t kPromptMaxStride = 1 << 24;   // bytes between tokens: 64 rows
 void launch_window_prompt(const AttendArgs &a, int head_dim, int max_rows, hipStream_t stream);
 
 // Joins the splits' outputs, and adds to the weights if a.accumulate.
-void launch_attend_join(const AttendArgs &a, AttendSource source, bool f32, int head_dim,
+void launch_attend_join(AttendArgs a, AttendSource source, bool f32, int head_dim,
                         int max_rows, hipStream_t stream);
 
 // Row tiles per workgroup for that many rows, and workgroups to split `keys` keys

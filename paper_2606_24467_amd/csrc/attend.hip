@@ -12,65 +12,79 @@
 
 namespace ckv {
 
-// A row's reference and 1 / sum (0: it saw nothing) over its splits, by one wave: a lane
-// per split, then butterflies.
-__device__ __forceinline__ float2 join_row(const float2 *ml, int64_t stride, int splits, int lane) {
-  float2 x[kAttendMaxSplits / 64];
-  float top = -INFINITY;
+// References and 1 / sum (0: it saw nothing) over the splits of `rows` rows, the first at
+// global row r0 of the group, into row_s: 2^k lanes per row (at least one per
+// split, up to 64), all rows' loads under way together.
+__device__ __forceinline__ void join_rows(const AttendArgs &a, int64_t slot0, int r0, int rows, float2 *row_s) {
+  const int RM = 16 * a.rt;
+  int lanes = 1;
+  while (lanes < a.splits && lanes < 64) lanes *= 2;
+  const int sub = (int)threadIdx.x & (lanes - 1);
+  for (int base = 0; base < rows; base += 256 / lanes) {   // uniform: every lane takes part in the butterflies
+    const int r = base + (int)threadIdx.x / lanes;
+    const int row = r0 + min(r, rows - 1), rb = row / RM;
+    const float2 *ml = a.part_ml + (slot0 + (int64_t)rb * a.splits) * RM + (row - rb * RM);
+    float2 x[kAttendMaxSplits / 64];
+    float top = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kAttendMaxSplits / 64; ++i) {
-    const int s = lane + 64 * i;
-    x[i] = s < splits ? ml[s * stride] : make_float2(-INFINITY, 0.f);
-    top = fmaxf(top, x[i].x);
+    for (int i = 0; i < kAttendMaxSplits / 64; ++i) {
+      const int s = sub + lanes * i;
+      x[i] = s < a.splits ? ml[(int64_t)s * RM] : make_float2(-INFINITY, 0.f);
+      top = fmaxf(top, x[i].x);
+    }
+    for (int o = lanes / 2; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kAttendMaxSplits / 64; ++i) sum += x[i].y * fast_exp2(x[i].x - ref);
+    for (int o = lanes / 2; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+    if (sub == 0 && r < rows) row_s[r] = make_float2(ref, sum == 0.f ? 0.f : 1.f / sum);
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < kAttendMaxSplits / 64; ++i) sum += x[i].y * fast_exp2(x[i].x - ref);
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
-  return make_float2(ref, sum == 0.f ? 0.f : 1.f / sum);
 }
 
 constexpr int64_t kOneKeys = 2048;
 constexpr int kJoinSlots = 1024;   // slots whose weights one workgroup adds to
 
 // Grid (out_blocks + weight blocks, groups), 256 threads.  The first out_blocks
-// join the splits' outputs, a row each: the splits are dealt to 1024 / D groups of
-// D / 4 lanes, whose sums are added in order.  Each of the others adds to the
+// join the splits' outputs, up to 1024 / D rows each: D / 4 lanes per row, and where
+// that leaves lanes (few rows, many splits) the splits are dealt to several such
+// parts, whose sums are added in order.  Each of the others adds to the
 // weights of kJoinSlots slots what the group's rows gave them, row by row in
 // order.  Bound by the latency of its few dependent loads.
 template <AttendSource SRC, typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, int out_blocks) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bg = blockIdx.y, RM = 16 * a.rt;
+  const int tid = threadIdx.x, bg = blockIdx.y, RM = 16 * a.rt;
   const int b = bg / a.Hkv, g = bg - b * a.Hkv;
   const int64_t slot0 = (int64_t)bg * a.row_blocks * a.splits;
   if ((int)blockIdx.x < out_blocks) {
-    constexpr int LR = D / 4, NP = 256 / LR;      // lanes per row, parts of the splits
+    constexpr int LR = D / 4, NP = 256 / LR;      // lanes per row; rows x parts of the splits
     __shared__ __align__(16) f32x4 part_s[NP][LR];
+    __shared__ float2 all_s[NP];
     const int q0 = SRC == kOverWindow ? a.cu_q[b] : 0;
     const int rows = SRC == kOverWindow ? (a.cu_q[b + 1] - q0) * a.G : a.rows;
-    const int r = blockIdx.x;
-    if (r >= rows) return;                        // uniform
-    const int rb = r / RM, rr = r - rb * RM, d = 4 * (tid % LR), part = tid / LR;
+    const int r0 = (int)blockIdx.x * a.join_rows;
+    if (r0 >= rows) return;                       // uniform
+    const int here = min(a.join_rows, rows - r0), parts = NP / a.join_rows;
+    join_rows(a, slot0, r0, here, all_s);
+    __syncthreads();
+    const int e = tid / LR, mine = e / parts, part = e % parts, d = 4 * (tid % LR);
+    const int r = r0 + min(mine, here - 1), rb = r / RM, rr = r - rb * RM;
+    const float2 all = all_s[min(mine, here - 1)];
     const float2 *ml = a.part_ml + (slot0 + (int64_t)rb * a.splits) * RM + rr;
-    const float2 all = join_row(ml, RM, a.splits, lane);
     const float *po = a.part_o + ((slot0 + (int64_t)rb * a.splits) * RM + rr) * D + d;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = part; s < a.splits; s += NP) {
+    for (int s = part; s < a.splits; s += parts) {
       const float f = fast_exp2(ml[(int64_t)s * RM].x - all.x);
       const f32x4 x = *reinterpret_cast<const f32x4 *>(po + (int64_t)s * RM * D);
 #pragma unroll
       for (int k = 0; k < 4; ++k) o[k] += x[k] * f;
     }
-    part_s[part][tid % LR] = o;
+    part_s[e][tid % LR] = o;
     __syncthreads();
-    if (part == 0) {
-      for (int p = 1; p < NP; ++p) {
-        const f32x4 x = part_s[p][tid % LR];
+    if (part == 0 && mine < here) {
+      for (int p = 1; p < parts; ++p) {
+        const f32x4 x = part_s[e + p][tid % LR];
 #pragma unroll
         for (int k = 0; k < 4; ++k) o[k] += x[k];
       }
@@ -86,15 +100,14 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, in
     const int n = live_slots(a.c, bg);
     const int s0 = ((int)blockIdx.x - out_blocks) * kJoinSlots;
     if (s0 >= n) return;                          // uniform
-    for (int r = wave; r < a.rows; r += 4) {
-      const int rb = r / RM, rr = r - rb * RM;
-      const float2 all = join_row(a.part_ml + (slot0 + (int64_t)rb * a.splits) * RM + rr, RM, a.splits, lane);
-      if (lane == 0) row_s[r] = all;
-    }
+    float got[kJoinSlots / 256] = {}, old[kJoinSlots / 256];
+#pragma unroll
+    for (int i = 0; i < kJoinSlots / 256; ++i)
+      old[i] = a.c.weight[(int64_t)bg * a.c.capacity + min(s0 + tid + 256 * i, n - 1)];
+    join_rows(a, slot0, 0, a.rows, row_s);
     __syncthreads();
-    float got[kJoinSlots / 256] = {};
     const float *z = a.logits + (int64_t)bg * a.rows * a.logit_stride;
-#pragma unroll 2
+#pragma unroll 4
     for (int r = 0; r < a.rows; ++r) {
       const float2 all = row_s[r];
 #pragma unroll
@@ -106,14 +119,17 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, in
 #pragma unroll
     for (int i = 0; i < kJoinSlots / 256; ++i) {
       const int s = s0 + tid + 256 * i;
-      if (s < n) a.c.weight[(int64_t)bg * a.c.capacity + s] += got[i];
+      if (s < n) a.c.weight[(int64_t)bg * a.c.capacity + s] = old[i] + got[i];
     }
   }
 }
 
-void launch_attend_join(const AttendArgs &a, AttendSource source, bool f32, int head_dim, int max_rows,
+void launch_attend_join(AttendArgs a, AttendSource source, bool f32, int head_dim, int max_rows,
                         hipStream_t stream) {
-  const int out_blocks = a.splits > 1 ? max_rows : 0;
+  // rows per workgroup: as many as fill it, fewer where the splits are many
+  a.join_rows = 1024 / head_dim;
+  while (a.join_rows > 1 && a.splits > 4 * (1024 / head_dim / a.join_rows)) a.join_rows /= 2;
+  const int out_blocks = a.splits > 1 ? (max_rows + a.join_rows - 1) / a.join_rows : 0;
   const int weight_blocks = a.accumulate && !a.one ? (a.c.capacity + kJoinSlots - 1) / kJoinSlots : 0;
   if (out_blocks + weight_blocks == 0) return;
   const dim3 grid(out_blocks + weight_blocks, a.c.groups);

@@ -6,8 +6,9 @@
 //   cache_append_kernel   new tokens' rows behind the live slots
 //   cache_len_kernel      ... and the lengths, where several workgroups append
 //   cache_read_kernel     rows as bf16 or fp32 values
-//   evict_select_kernel   which slots go, and which kept slots take their place
-//   evict_move_kernel     the moves
+//   evict_kernel          which slots go, which kept slots take their place, and
+//                         the moves, where they can only be few
+//   evict_move_kernel     the moves alone
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -141,11 +142,12 @@ struct AppendArgs {
   int32_t own_len;              // the group's one workgroup updates len and seen
 };
 
-// Grid (groups, blocks per group), 256 threads: a lane per 8 values of a K or
+// Grid (groups, blocks per group), 256 or 1024 threads: a lane per 8 values of a K or
 // V row.  Bound by latency at a decoding step's one token.
 template <typename T, int D, bool FP4>
-__global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
-  constexpr int U = D / 8, ROWS = 256 / (2 * U);   // tokens per workgroup and trip
+__global__ __launch_bounds__(1024) void cache_append_kernel(const AppendArgs a) {
+  constexpr int U = D / 8;
+  const int ROWS = (int)blockDim.x / (2 * U);      // tokens per workgroup and trip
   const int tid = threadIdx.x, bg = blockIdx.x;
   const int b = bg / a.c.Hkv, g = bg - b * a.c.Hkv;
   const int len = live_slots(a.c, bg);
@@ -232,9 +234,8 @@ __device__ __forceinline__ uint32_t evict_key(float w, int32_t pos, int32_t n_si
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
-
 // The sum of one int per wave over the waves before this one, and over all.
+template <int NW>
 __device__ __forceinline__ int wave_prefix(int mine, int wave, int lane, int *lds, int &total) {
   __syncthreads();
   if (lane == 0) lds[wave] = mine;
@@ -242,128 +243,299 @@ __device__ __forceinline__ int wave_prefix(int mine, int wave, int lane, int *ld
   int before = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kEvictWaves; ++w) {
+  for (int w = 0; w < NW; ++w) {
     before += w < wave ? lds[w] : 0;
     total += lds[w];
   }
   return before;
 }
 
-// One workgroup per group: the key of the (len - budget)-th smallest slot by
-// radix select (11 + 11 + 10 bits, histograms in LDS), then, every wave on a
-// consecutive run of slots, the freed slots below the budget and the kept ones
-// from it on, both in ascending order by ballots and prefix sums.
-__global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const EvictArgs a) {
-  __shared__ int hist[2048];
-  __shared__ int sums[kEvictWaves];
-  __shared__ int pick[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, bg = blockIdx.x;
+// A move: the lanes of a wave copy 16 bytes each of the K and the V row (at most
+// 512 bytes each), four of them the rest.  No slot is both read and written (from
+// >= budget > to).
+__device__ __forceinline__ void move_slot(const EvictArgs &a, int64_t to, int64_t from, int lane) {
+  const int units = a.row_bytes / 16;
+  if (lane < 2 * units) {
+    char *rows = lane < units ? a.c.k : a.c.v;
+    const int u = lane < units ? lane : lane - units;
+    store16(to_global(rows) + to * a.row_bytes + 16 * u,
+            load16(to_global(rows) + from * a.row_bytes + 16 * u));
+  }
+  if (lane < a.scale_bytes) {
+    a.c.k_scale[to * a.scale_bytes + lane] = a.c.k_scale[from * a.scale_bytes + lane];
+    a.c.v_scale[to * a.scale_bytes + lane] = a.c.v_scale[from * a.scale_bytes + lane];
+  }
+  if (lane == 0) a.c.pos[to] = a.c.pos[from];
+  if (lane == 1) a.c.weight[to] = a.c.weight[from];
+}
+
+constexpr int kFusedMoves = 256;    // moves that evict_kernel makes itself, at most
+constexpr int kEvictList = 512;     // keys that it ranks against each other, at most
+
+// The key of the last of the `drop` slots that go, and how many keys lie below it: two
+// bits at a time from the top, by counting the keys below three candidates (each
+// wave's by ballots, then one LDS counter each).  No histogram: the weights have
+// few exponents, and all of them would meet in a few bins.  count(t1, t2, t3, n): the
+// wave's keys below each.  counters [16][4] are zero.
+// STEPS < 16: the top 2 STEPS bits alone.
+template <int STEPS, typename F>
+__device__ __forceinline__ uint32_t search_key(F &&count, int (*counters)[4], int drop, int lane, int &less) {
+  uint32_t t = 0;
+  less = 0;
+#pragma unroll 1
+  for (int step = 0; step < STEPS; ++step) {
+    const int bit = 30 - 2 * step;
+    int n[3] = {0, 0, 0};
+    count(t | 1u << bit, t | 2u << bit, t | 3u << bit, n);
+    if (lane < 3) atomicAdd(&counters[step][lane], lane == 0 ? n[0] : lane == 1 ? n[1] : n[2]);
+    __syncthreads();
+    const int c1 = counters[step][0], c2 = counters[step][1], c3 = counters[step][2];
+    if (c3 < drop) t |= 3u << bit, less = c3;
+    else if (c2 < drop) t |= 2u << bit, less = c2;
+    else if (c1 < drop) t |= 1u << bit, less = c1;
+  }
+  return t;
+}
+
+// One workgroup of NT threads per group, each wave on a consecutive run of its slots.
+// One slot to drop, the case of a decoding step: one look at the weights, the
+// smallest (key, highest slot) by butterflies, and at most one move.
+// Up to 256: the threads' smallest keys bound the drop-th smallest of all (its top
+// 14 bits are searched for: a float to 3%), and the few (key, slot) below the bound
+// are ranked against each other in LDS; so are the freed slots, for their order.
+// Else, or where too many keys are alike: search_key over all keys (in LDS, up to
+// LKEYS of them; else read anew each time), then the freed slots below the budget
+// and the kept ones from it on, both ascending, by ballots and prefix sums.
+// FUSED: the moves too; else their lists go to the workspace.
+// Loops stay loops: unrolled over a thread's keys in registers, the code that each
+// workgroup runs once took longer to fetch than to run.
+template <int NT, int LKEYS, bool FUSED>
+__global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
+  constexpr int NW = NT / 64;
+  static_assert(LKEYS % (4 * NT) == 0, "a thread's keys come in fours");
+  __shared__ int count_s[2][16][4];
+  __shared__ uint64_t least_s[NW];
+  __shared__ int sums[NW];
+  __shared__ int2 pairs[NW];
+  __shared__ int to_s[FUSED ? kFusedMoves : 1], from_s[FUSED ? kFusedMoves : 1];
+  __shared__ uint64_t list_s[kEvictList];   // key << 32 | ~slot: the first ones go first
+  __shared__ int freed_s[kEvictList];       // of each, its slot if it is freed below the budget
+  __shared__ uint8_t tail_gone_s[kFusedMoves];
+  __shared__ uint32_t keys_s[LKEYS ? LKEYS : 1];
+  __shared__ int listed_s, moves_s;
+  const int tid = threadIdx.x, lane = tid & 63, bg = blockIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = live_slots(a.c, bg);
   if (n <= a.budget) {           // uniform
-    if (tid == 0) a.count[bg] = 0;
+    if (!FUSED && tid == 0) a.count[bg] = 0;
     return;
   }
   const int64_t base = (int64_t)bg * a.c.capacity;
   const float *weight = a.c.weight + base;
   const int32_t *pos = a.c.pos + base;
   const int64_t recent_from = (int64_t)a.c.seen[bg] - a.n_recent;
-  auto key_of = [&](int s) { return evict_key(weight[s], pos[s], a.n_sinks, recent_from); };
-  int left = n - a.budget;       // to drop among the keys that share `prefix`
-  uint32_t prefix = 0, mask = 0;
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < 2048; i += kEvictThreads) hist[i] = 0;
-    __syncthreads();
-    for (int s = tid; s < n; s += kEvictThreads) {
-      const uint32_t key = key_of(s);
-      if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & ((1u << bits) - 1)], 1);
+  const int nj = (n + 4 * NT - 1) / (4 * NT) * 4;           // keys of a thread, in fours
+  const int first = wave * 64 * nj + lane;                  // its slots: first + 64 j
+  auto read_key = [&](int slot) {                           // past the end: below no candidate
+    const int s = min(slot, n - 1);
+    const uint32_t k = evict_key(weight[s], pos[s], a.n_sinks, recent_from);
+    return slot < n ? k : 0xFFFFFFFFu;
+  };
+  const int drop = n - a.budget;
+  int moves = 0;
+  if (drop == 1) {
+    uint64_t least = ~0ull;
+#pragma unroll 8
+    for (int j = 0; j < nj; ++j) {
+      const int slot = first + 64 * j;
+      const uint64_t k = (uint64_t)read_key(slot) << 32 | (uint32_t)~slot;
+      if (slot < n) least = min(least, k);
     }
-    __syncthreads();
-    if (wave == 0) {             // the digit at which the running count reaches `left`
-      int mine = 0;
-      for (int i = 0; i < 32; ++i) mine += hist[32 * lane + i];
-      int upto = mine;
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int t = __shfl_up(upto, o);
-        if (lane >= o) upto += t;
+    for (int o = 32; o >= 1; o >>= 1) least = min(least, (uint64_t)__shfl_xor((unsigned long long)least, o));
+    if (lane == 0) least_s[wave] = least;
+    __syncthreads();
+    if (wave) return;            // uniform; no barrier follows on this path
+#pragma unroll
+    for (int w = 0; w < NW; ++w) least = min(least, least_s[w]);
+    const int gone = (int)~(uint32_t)least;
+    if (lane == 0) {
+      if constexpr (!FUSED) {
+        a.count[bg] = gone < a.budget ? 1 : 0;
+        a.to[bg * a.stride] = gone;
+        a.from[bg * a.stride] = a.budget;
       }
-      if (upto >= left && upto - mine < left) {   // one lane
-        int run = upto - mine, d = 32 * lane;
-        while (run + hist[d] < left) run += hist[d++];
-        pick[0] = d;
-        pick[1] = run;
+      a.c.len[bg] = a.budget;
+    }
+    // by the one slot from the budget on
+    if (FUSED && gone < a.budget) move_slot(a, base + gone, base + a.budget, lane);
+    return;
+  }
+  uint32_t least = 0xFFFFFFFFu;
+#pragma unroll 8
+  for (int j = 0; j < nj; ++j) {
+    const uint32_t k = read_key(first + 64 * j);
+    least = min(least, k);
+    if (LKEYS) keys_s[tid + NT * j] = k;         // read by this thread alone
+  }
+  // keys j .. j + 3, together
+  auto keys_at = [&](int j, uint32_t (&k)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) k[e] = LKEYS ? keys_s[tid + NT * (j + e)] : read_key(first + 64 * (j + e));
+  };
+  if (tid < 128) reinterpret_cast<int *>(count_s)[tid] = 0;
+  if (tid == 0) listed_s = 0;
+  __syncthreads();
+  uint32_t t = 0;                // the key of the last slot that goes
+  int less = 0;                  // keys below it
+  if (drop <= kFusedMoves && drop <= NT / 2) {
+    auto count_least = [&](uint32_t t1, uint32_t t2, uint32_t t3, int (&c)[3]) {
+      c[0] = __popcll(__ballot(least < t1));
+      c[1] = __popcll(__ballot(least < t2));
+      c[2] = __popcll(__ballot(least < t3));
+    };
+    uint32_t bound = 0xFFFFFFFFu;                // (all keys but the held slots')
+    if (n > kEvictList) {
+      bound = search_key<7>(count_least, count_s[0], drop, lane, less) + (1u << 18);
+      if (bound == 0u) bound = 0xFFFFFFFFu;
+    }
+    for (int j = 0; j < nj; j += 4) {
+      uint32_t k[4];
+      keys_at(j, k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (k[e] < bound) {
+          const int i = atomicAdd(&listed_s, 1);
+          if (i < kEvictList) list_s[i] = (uint64_t)k[e] << 32 | (uint32_t)~(first + 64 * (j + e));
+        }
+    }
+    if (tid < kFusedMoves) tail_gone_s[tid] = 0;
+    __syncthreads();
+    const int listed = listed_s;
+    if (listed >= drop && listed <= kEvictList) {   // uniform
+      for (int i = tid; i < listed; i += NT) {
+        const uint64_t mine = list_s[i];
+        int rank = 0;
+#pragma unroll 8
+        for (int o = 0; o < listed; ++o) rank += list_s[o] < mine;
+        const int slot = (int)~(uint32_t)mine;
+        const bool gone = rank < drop;
+        freed_s[i] = gone && slot < a.budget ? slot : INT32_MAX;
+        if (gone && slot >= a.budget) tail_gone_s[slot - a.budget] = 1;
+      }
+      __syncthreads();
+      int32_t *to = FUSED ? to_s : a.to + bg * a.stride, *from = FUSED ? from_s : a.from + bg * a.stride;
+      for (int i = tid; i < listed; i += NT) {
+        const int mine = freed_s[i];
+        int rank = 0;
+#pragma unroll 8
+        for (int o = 0; o < listed; ++o) rank += freed_s[o] < mine;
+        if (mine != INT32_MAX) to[rank] = mine;
+      }
+      if (wave == 0) {
+        int kept = 0;
+        for (int x = 0; x < drop; x += 64) {
+          const bool tail = x + lane < drop && !tail_gone_s[x + lane];
+          const uint64_t m = __ballot(tail);
+          if (tail) from[kept + __popcll(m & ((1ull << lane) - 1))] = a.budget + x + lane;
+          kept += __popcll(m);
+        }
+        if (lane == 0) {
+          moves_s = kept;        // as many as freed slots: drop of n - budget slots stay behind
+          if constexpr (!FUSED) a.count[bg] = kept;
+          a.c.len[bg] = a.budget;
+        }
+      }
+      if constexpr (FUSED) {
+        __syncthreads();
+        for (int m = wave; m < moves_s; m += NW) move_slot(a, base + to_s[m], base + from_s[m], lane);
+      }
+      return;
+    }
+  }
+  auto count_all = [&](uint32_t t1, uint32_t t2, uint32_t t3, int (&c)[3]) {
+    for (int j = 0; j < nj; j += 4) {
+      uint32_t k[4];
+      keys_at(j, k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        c[0] += __popcll(__ballot(k[e] < t1));
+        c[1] += __popcll(__ballot(k[e] < t2));
+        c[2] += __popcll(__ballot(k[e] < t3));
       }
     }
-    __syncthreads();
-    prefix |= (uint32_t)pick[0] << shift;
-    mask |= ((1u << bits) - 1) << shift;
-    left -= pick[1];
-  }
-  // keys below `prefix` go, and the `left` highest slots of those equal to it
-  const int run = ((n + kEvictWaves - 1) / kEvictWaves + 63) / 64 * 64;
-  const int s0 = min(n, wave * run), s1 = min(n, s0 + run);
+  };
+  t = search_key<16>(count_all, count_s[1], drop, lane, less);
+  // keys below t go, and the highest slots of those equal to it
   int equal = 0;
-  for (int s = s0; s < s1; s += 64)
-    equal += __popcll(__ballot(s + lane < s1 && key_of(min(s + lane, n - 1)) == prefix));
+  for (int j = 0; j < nj; j += 4) {
+    uint32_t k[4];
+    keys_at(j, k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) equal += __popcll(__ballot(k[e] == t && first + 64 * (j + e) < n));
+  }
   int all_equal;
-  const int equal_before = wave_prefix(equal, wave, lane, sums, all_equal);
-  const int keep_equal = all_equal - left;
+  const int equal_before = wave_prefix<NW>(equal, wave, lane, sums, all_equal);
+  const int keep_equal = all_equal - (drop - less);
   const uint64_t below = (1ull << lane) - 1;
-  int holes = 0, tails = 0, hole0 = 0, tail0 = 0, unused;
-  for (int pass = 0; pass < 2; ++pass) {          // count, then write
+  int2 at = make_int2(0, 0);     // freed slots and kept tails before this wave's
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {         // count, then write
     int eq = equal_before, nh = 0, nt = 0;
-    for (int s = s0; s < s1; s += 64) {
-      const int slot = s + lane;
-      const bool in = slot < s1;
-      const uint32_t key = key_of(min(slot, n - 1));
-      const uint64_t eq_m = __ballot(in && key == prefix);
-      const bool gone = key < prefix || (key == prefix && eq + __popcll(eq_m & below) >= keep_equal);
-      eq += __popcll(eq_m);
-      const bool hole = in && gone && slot < a.budget, tail = in && !gone && slot >= a.budget;
-      const uint64_t h_m = __ballot(hole), t_m = __ballot(tail);
-      if (pass == 1) {
-        if (hole) a.to[bg * a.stride + hole0 + nh + __popcll(h_m & below)] = slot;
-        if (tail) a.from[bg * a.stride + tail0 + nt + __popcll(t_m & below)] = slot;
+#pragma unroll 1
+    for (int j = 0; j < nj; j += 4) {
+      uint32_t k[4];
+      keys_at(j, k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int slot = first + 64 * (j + e);
+        const bool in = slot < n;
+        const uint64_t eq_m = __ballot(in && k[e] == t);
+        const bool gone = k[e] < t || (k[e] == t && eq + __popcll(eq_m & below) >= keep_equal);
+        eq += __popcll(eq_m);
+        const bool hole = in && gone && slot < a.budget, tail = in && !gone && slot >= a.budget;
+        const uint64_t h_m = __ballot(hole), t_m = __ballot(tail);
+        if (pass == 1) {
+          const int h = at.x + nh + __popcll(h_m & below), l = at.y + nt + __popcll(t_m & below);
+          if constexpr (FUSED) {
+            if (hole) to_s[h] = slot;
+            if (tail) from_s[l] = slot;
+          } else {
+            if (hole) a.to[bg * a.stride + h] = slot;
+            if (tail) a.from[bg * a.stride + l] = slot;
+          }
+        }
+        nh += __popcll(h_m);
+        nt += __popcll(t_m);
       }
-      nh += __popcll(h_m);
-      nt += __popcll(t_m);
     }
     if (pass == 0) {
-      hole0 = wave_prefix(nh, wave, lane, sums, holes);
-      tail0 = wave_prefix(nt, wave, lane, sums, unused);
-      tails = unused;
+      if (lane == 0) pairs[wave] = make_int2(nh, nt);
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const int2 x = pairs[w];
+        if (w < wave) at.x += x.x, at.y += x.y;
+        moves += x.x;
+      }
     }
   }
-  (void)tails;                   // as many as holes: n - drop = budget slots stay
   if (tid == 0) {
-    a.count[bg] = holes;
+    if constexpr (!FUSED) a.count[bg] = moves;
     a.c.len[bg] = a.budget;
+  }
+  if constexpr (FUSED) {
+    __syncthreads();
+    for (int m = wave; m < moves; m += NW) move_slot(a, base + to_s[m], base + from_s[m], lane);
   }
 }
 
-// Grid (groups, blocks), a wave per move: the lanes copy 16 bytes each of the
-// K and the V row (at most 512 bytes each), four of them the rest.  No slot is
-// both read and written (from >= budget > to).
+// Grid (groups, blocks), a wave per move.
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs a) {
-  const int lane = threadIdx.x & 63, bg = blockIdx.x;
-  const int n = a.count[bg], units = a.row_bytes / 16;
+  const int lane = threadIdx.x & 63, bg = blockIdx.x, n = a.count[bg];
   const int64_t base = (int64_t)bg * a.c.capacity;
-  for (int m = (int)blockIdx.y * 4 + ((int)threadIdx.x >> 6); m < n; m += 4 * (int)gridDim.y) {
-    const int64_t to = base + a.to[bg * a.stride + m], from = base + a.from[bg * a.stride + m];
-    if (lane < 2 * units) {
-      char *rows = lane < units ? a.c.k : a.c.v;
-      const int u = lane < units ? lane : lane - units;
-      store16(to_global(rows) + to * a.row_bytes + 16 * u,
-              load16(to_global(rows) + from * a.row_bytes + 16 * u));
-    }
-    if (lane < a.scale_bytes) {
-      a.c.k_scale[to * a.scale_bytes + lane] = a.c.k_scale[from * a.scale_bytes + lane];
-      a.c.v_scale[to * a.scale_bytes + lane] = a.c.v_scale[from * a.scale_bytes + lane];
-    }
-    if (lane == 0) a.c.pos[to] = a.c.pos[from];
-    if (lane == 1) a.c.weight[to] = a.c.weight[from];
-  }
+  for (int m = (int)blockIdx.y * 4 + ((int)threadIdx.x >> 6); m < n; m += 4 * (int)gridDim.y)
+    move_slot(a, base + a.to[bg * a.stride + m], base + a.from[bg * a.stride + m], lane);
 }
 
 }  // namespace ckv
@@ -498,13 +670,13 @@ int compresskv_cache_append(const ckv_cache *c, int32_t dtype, int32_t n_new, co
   a.k = static_cast<const char *>(k_new);
   a.v = static_cast<const char *>(v_new);
   a.n_new = n_new;
-  // one workgroup per group takes up to four trips, and the lengths with them
-  const int rows = 256 / (2 * c->head_dim / 8);
-  const int64_t trips = ((int64_t)n_new + rows - 1) / rows;
-  a.own_len = trips <= 4;
-  const unsigned per_group = a.own_len ? 1u : (unsigned)std::min<int64_t>((trips + 3) / 4, 1024);
+  // one workgroup per group takes up to eight trips, and the lengths with them
+  const int threads = n_new * 2 * (c->head_dim / 8) <= 256 ? 256 : 1024;
+  const int64_t rows = threads / (2 * (c->head_dim / 8)), trips = (n_new + rows - 1) / rows;
+  a.own_len = trips <= 8;
+  const unsigned per_group = a.own_len ? 1u : (unsigned)std::min<int64_t>((trips + 7) / 8, 1024);
   with_rows(c, dtype, [&]<typename T, int D, bool FP4>() {
-    hipLaunchKernelGGL((ckv::cache_append_kernel<T, D, FP4>), dim3(a.c.groups, per_group), dim3(256),
+    hipLaunchKernelGGL((ckv::cache_append_kernel<T, D, FP4>), dim3(a.c.groups, per_group), dim3(threads),
                        0, (hipStream_t)stream, a);
   });
   if (!a.own_len) {
@@ -566,8 +738,19 @@ int compresskv_cache_evict(const ckv_cache *c, int32_t budget, int32_t n_sinks, 
   a.n_recent = n_recent;
   a.row_bytes = ckv_api::row_bytes(c);
   a.scale_bytes = c->dtype == CKV_FP4 ? c->head_dim / 32 : 0;
-  hipLaunchKernelGGL(ckv::evict_select_kernel, dim3(a.c.groups), dim3(ckv::kEvictThreads), 0,
-                     (hipStream_t)stream, a);
+  const bool fused = a.stride <= ckv::kFusedMoves;
+  auto go = [&]<int NT, int LKEYS>() {
+    if (fused)
+      hipLaunchKernelGGL((ckv::evict_kernel<NT, LKEYS, true>), dim3(a.c.groups), dim3(NT), 0,
+                         (hipStream_t)stream, a);
+    else
+      hipLaunchKernelGGL((ckv::evict_kernel<NT, LKEYS, false>), dim3(a.c.groups), dim3(NT), 0,
+                         (hipStream_t)stream, a);
+  };
+  if (c->capacity <= 8192) go.template operator()<256, 8192>();
+  else if (c->capacity <= 36864) go.template operator()<1024, 36864>();
+  else go.template operator()<1024, 0>();
+  if (fused) return launched("cache evict");
   if ((st = launched("cache evict"))) return st;
   const unsigned per_group = (unsigned)std::min<int64_t>((a.stride + 31) / 32, 64);
   hipLaunchKernelGGL(ckv::evict_move_kernel, dim3(a.c.groups, per_group), dim3(256), 0,
