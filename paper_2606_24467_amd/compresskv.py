@@ -644,13 +644,19 @@ def compress_layer_heads(p: Problem, q_win, k, v, srh_mask, group_budgets, *, wa
 # ---------------------------------------------------------------------------
 # The bounded cache and the windowed attention (include/compresskv_cache.h)
 # ---------------------------------------------------------------------------
+_I64x3 = ctypes.c_int64 * 3
+_NO_CONTEXT = contextlib.nullcontext()
+
+
 def _enter(device: torch.device, stream):
-    """(context, stream handle) of a call on the tensors' device: temporaries and
-    outputs are allocated on the stream that the call runs on."""
+    """(context, stream handle) of a call on the tensors' device: temporaries and outputs
+    are allocated on the stream that the call runs on.  (A decoding step makes
+    several of these calls: the raw handle is asked for, not a Stream object.)"""
     if stream is None:
-        here = torch.cuda.current_device() == device.index
-        return (contextlib.nullcontext() if here else torch.cuda.device(device),
-                torch.cuda.current_stream(device).cuda_stream)
+        index = device.index
+        here = torch.cuda.current_device() == index
+        return (_NO_CONTEXT if here else torch.cuda.device(device),
+                torch._C._cuda_getCurrentRawStream(index))
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
     if stream.device != device:
@@ -769,22 +775,22 @@ class Cache:
 
     def append(self, k_new, v_new, stream=None) -> None:
         """New tokens' rows [batch, n, Hkv, D], D contiguous."""
-        for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-            if (t.dim() != 4 or t.shape[0] != self.batch or t.shape[2] != self.n_kv_heads
-                    or t.shape[3] != self.head_dim or t.shape != k_new.shape):
-                raise ValueError(f"{name} must be [batch, n, Hkv, D]")
-            if t.dtype != k_new.dtype:
-                raise ValueError("k_new and v_new must share one dtype")
-            if t.stride(3) != 1:
-                raise ValueError(f"the head dimension of {name} must be contiguous")
-            if t.device != self.device:
-                raise ValueError(f"{name} must be on {self.device}")
-        strides = [(ctypes.c_int64 * 3)(*t.stride()[:3]) for t in (k_new, v_new)]
+        shape, dtype = k_new.shape, k_new.dtype
+        if (len(shape) != 4 or v_new.shape != shape or shape[0] != self.batch
+                or shape[2] != self.n_kv_heads or shape[3] != self.head_dim):
+            raise ValueError("k_new and v_new must be [batch, n, Hkv, D]")
+        if v_new.dtype != dtype:
+            raise ValueError("k_new and v_new must share one dtype")
+        ks, vs = k_new.stride(), v_new.stride()
+        if ks[3] != 1 or vs[3] != 1:
+            raise ValueError("the head dimension of k_new and v_new must be contiguous")
+        if k_new.device != self.device or v_new.device != self.device:
+            raise ValueError(f"k_new and v_new must be on {self.device}")
         ctx, handle = _enter(self.device, stream)
         with ctx:
             _check("compresskv_cache_append", lib().compresskv_cache_append(
-                self._ref, _row_dtype(k_new.dtype), k_new.shape[1], k_new.data_ptr(), strides[0],
-                v_new.data_ptr(), strides[1], handle))
+                self._ref, _row_dtype(dtype), shape[1], k_new.data_ptr(), _I64x3(*ks[:3]),
+                v_new.data_ptr(), _I64x3(*vs[:3]), handle))
 
     def read(self, dtype: torch.dtype | None = None, stream=None):
         """(k, v) [batch, Hkv, capacity, D] as values, zeros past the live slots."""

@@ -56,6 +56,8 @@ __device__ __forceinline__ void add_unbounded(f32x4 &acc, f32x4 up, f32x4 down, 
   }
 }
 
+constexpr int64_t kNearStride = 1 << 24;   // bytes between rows: 64 of them stay within 32 bits
+
 template <CacheType CT, int D>
 struct AttendShape {
   static constexpr int NT = CT == kCacheF32 ? 1 : 2;     // 16-key tiles per step
@@ -92,8 +94,8 @@ template <AttendSource SRC, CacheType CT, int D, int RT, int QP, bool MASKS, boo
 __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kernel(const AttendArgs a) {
   constexpr int NW = (ONE ? 2 : 1) * kAttendWaves, NTH = 64 * NW;
   // steps whose rows are in registers or under way, as many as the registers hold
-  constexpr int DEPTH = (ONE && MASKS) || (CT == kCacheF32 && RT == 4) ? 1
-                        : CT == kCacheFp4 && QP == 1 ? 3 : 2;
+  constexpr int DEPTH = (ONE && MASKS) || (CT != kCacheFp4 && RT >= 2) ? 1
+                        : 2;
   using S = AttendShape<CT, D>;
   constexpr bool F32Q = CT == kCacheF32 || QP == 3;
   constexpr int NT = S::NT, KS = S::KS, NK = S::NK, DL = S::DL, VW = S::VW;
@@ -145,6 +147,125 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
       return base + (int64_t)(q0 + i) * a.q_tok + h * a.q_head;
   };
 
+  // positions of the lane's rows (row tile rt, column c); rows past the end as the last
+  int t_row[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = min(rb * RM + 16 * rt + c, rows - 1);
+    if constexpr (SRC == kOverCache) t_row[rt] = t_first + r / a.G;
+    else t_row[rt] = t_first - rb * RM / a.G + r / a.G;
+  }
+
+  // row bases
+  const char *kb, *vb;
+  int64_t k_row, v_row;
+  if constexpr (SRC == kOverCache) {
+    k_row = v_row = CT == kCacheFp4 ? D / 2 : D * (CT == kCacheF32 ? 4 : 2);
+    kb = a.c.k + (int64_t)bg * a.c.capacity * k_row;
+    vb = a.c.v + (int64_t)bg * a.c.capacity * v_row;
+  } else {
+    k_row = a.k_tok;
+    v_row = a.v_tok;
+    kb = a.k + k0 * a.k_tok + g * a.k_head;
+    vb = a.v + k0 * a.v_tok + g * a.v_head;
+  }
+  // Bytes that a lane takes of a K row (16 each) and of a V row, and its places in
+  // the first tile of a step: offsets in 32 bits, to a base that all lanes share.
+  constexpr int VB = CT == kCacheFp4 ? DL / 2 : DL * (CT == kCacheF32 ? 4 : 2);
+  constexpr int KB = CT == kCacheFp4 ? D / 8 : 16;
+  const bool near = SRC == kOverCache || (k_row <= kNearStride && v_row <= kNearStride);
+  const uint32_t k_off = near ? (uint32_t)(c * (int)k_row + KB * quad) : 0;
+  const uint32_t v_off = near ? (uint32_t)(4 * quad * (int)v_row + VB * c) : 0;
+  auto load_k = [&](gptr<const char> p, uint4 (&k)[CT == kCacheFp4 ? 1 : NK]) {
+    if constexpr (CT == kCacheFp4 && D == 64) {
+      const uint64_t h = *reinterpret_cast<gptr<const uint64_t>>(p);
+      k[0] = make_uint4((uint32_t)h, (uint32_t)(h >> 32), 0, 0);
+    } else if constexpr (CT == kCacheFp4) {
+      k[0] = load16(p);
+    } else {
+#pragma unroll
+      for (int s = 0; s < NK; ++s) k[s] = load16(p + 64 * s);
+    }
+  };
+  auto load_v = [&](gptr<const char> p, uint32_t (&v)[VW]) {
+    if constexpr (VB == 2) {
+      v[0] = *reinterpret_cast<gptr<const uint16_t>>(p);
+    } else if constexpr (VB == 4) {
+      v[0] = *reinterpret_cast<gptr<const uint32_t>>(p);
+    } else if constexpr (VB == 8) {
+      const uint64_t h = *reinterpret_cast<gptr<const uint64_t>>(p);
+      v[0] = (uint32_t)h, v[VW - 1] = (uint32_t)(h >> 32);
+    } else {
+#pragma unroll
+      for (int u = 0; u < VB / 16; ++u) {
+        const uint4 h = load16(p + 16 * u);
+        v[4 * u] = h.x, v[4 * u + 1] = h.y, v[4 * u + 2] = h.z, v[4 * u + 3] = h.w;
+      }
+    }
+  };
+
+  // Loads of step st (uniform).  Of a cache any slot can be read, dead ones too; past
+  // the last one, and past the last key of a window, the last one is.
+  const int end = SRC == kOverCache ? a.c.capacity : n;
+  auto load = [&](int st, AttendRaw<CT, D> &w) {
+    const int base = st * KS;
+    if (CT == kCacheFp4 || (near && base + KS <= end && base >= sinks)) {   // uniform: a run of rows
+      const char *kt = kb + (int64_t)(base - sinks + lo) * k_row, *vt = vb + (int64_t)(base - sinks + lo) * v_row;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        load_k(to_global(kt + 16 * t * k_row) + k_off, w.k[t]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_v(to_global(vt + (16 * t + i) * v_row) + v_off, w.v[t][i]);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        load_k(to_global(kb) + key_of(min(base + 16 * t + c, end - 1)) * k_row + KB * quad, w.k[t]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          load_v(to_global(vb) + key_of(min(base + 16 * t + 4 * quad + i, end - 1)) * v_row + VB * c, w.v[t][i]);
+      }
+    }
+    if constexpr (CT == kCacheFp4) {
+      const int64_t slot0 = (int64_t)bg * a.c.capacity + base;
+      const uint8_t *ks = a.c.k_scale + slot0 * (D / 32), *vs = a.c.v_scale + slot0 * (D / 32);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        w.ks[t] = (to_global(ks + 16 * t * (D / 32)))[(uint32_t)(c * (D / 32) + (D == 128 ? quad : quad >> 1))];
+        const gptr<const char> p = to_global(reinterpret_cast<const char *>(vs) + 16 * t * (D / 32)) +
+                                   (uint32_t)(4 * quad * (D / 32));
+        if constexpr (D == 128) {
+          const uint4 h = load16(p);
+          w.vs[t][0] = h.x, w.vs[t][1] = h.y, w.vs[t][2] = h.z, w.vs[t][3] = h.w;
+        } else {
+          const uint64_t h = *reinterpret_cast<gptr<const uint64_t>>(p);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w.vs[t][i] = (uint32_t)(h >> (16 * i)) & 0xFFFFu;
+        }
+      }
+    }
+    if constexpr (MASKS && SRC == kOverCache) {
+      const gptr<const int32_t> p = to_global(a.c.pos + (int64_t)bg * a.c.capacity);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int s = base + 16 * t + 4 * quad;
+        w.pos[t] = make_int4(p[min(s, end - 1)], p[min(s + 1, end - 1)], p[min(s + 2, end - 1)],
+                             p[min(s + 3, end - 1)]);
+      }
+    }
+  };
+
+  // the first steps' loads, before everything else that waits for memory; in one
+  // workgroup they do not depend on the length
+  AttendRaw<CT, D> w[DEPTH];
+  {
+    const int first = ONE && SRC == kOverCache ? wave : st0 + wave;
+    const int stop = ONE && SRC == kOverCache ? (a.c.capacity + KS - 1) / KS : st1;
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i)
+      if (first + i * NW < stop) load(first + i * NW, w[i]);
+  }
+
   AttendQ<CT, D, RT, QP> q;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -178,95 +299,6 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
       }
     }
   }
-  // positions of the lane's rows (row tile rt, column c); rows past the end as the last
-  int t_row[RT];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int r = min(rb * RM + 16 * rt + c, rows - 1);
-    if constexpr (SRC == kOverCache) t_row[rt] = t_first + r / a.G;
-    else t_row[rt] = t_first - rb * RM / a.G + r / a.G;
-  }
-
-  // row bases
-  const char *kb, *vb;
-  int64_t k_row, v_row;
-  if constexpr (SRC == kOverCache) {
-    k_row = v_row = CT == kCacheFp4 ? D / 2 : D * (CT == kCacheF32 ? 4 : 2);
-    kb = a.c.k + (int64_t)bg * a.c.capacity * k_row;
-    vb = a.c.v + (int64_t)bg * a.c.capacity * v_row;
-  } else {
-    k_row = a.k_tok;
-    v_row = a.v_tok;
-    kb = a.k + k0 * a.k_tok + g * a.k_head;
-    vb = a.v + k0 * a.v_tok + g * a.v_head;
-  }
-  const gptr<const char> kg = to_global(kb), vg = to_global(vb);
-
-  // Loads of step st.  Keys past the end read a key that exists (4-bit rows:
-  // the slots up to the next multiple of 32, which the capacity is).
-  auto load = [&](int st, AttendRaw<CT, D> &w) {
-    const int base = st * KS;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      if constexpr (CT == kCacheFp4) {
-        const int64_t slot0 = (int64_t)bg * a.c.capacity + base + 16 * t;
-        const gptr<const char> p = kg + (int64_t)(base + 16 * t + c) * (D / 2) + (D / 8) * quad;
-        if constexpr (D == 128) {
-          w.k[t][0] = load16(p);
-        } else {
-          const uint2 h = __builtin_bit_cast(uint2, *reinterpret_cast<gptr<const uint64_t>>(p));
-          w.k[t][0] = make_uint4(h.x, h.y, 0, 0);
-        }
-        w.ks[t] = to_global(a.c.k_scale)[(slot0 + c) * (D / 32) + (D == 128 ? quad : quad >> 1)];
-        const gptr<const char> sp = reinterpret_cast<gptr<const char>>(
-            to_global((const char *)a.c.v_scale) + (slot0 + 4 * quad) * (D / 32));
-        if constexpr (D == 128) {
-          const uint4 h = load16(sp);
-          w.vs[t][0] = h.x, w.vs[t][1] = h.y, w.vs[t][2] = h.z, w.vs[t][3] = h.w;
-        } else {
-          const uint64_t h = *reinterpret_cast<gptr<const uint64_t>>(sp);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w.vs[t][i] = (uint32_t)(h >> (16 * i)) & 0xFFFFu;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const gptr<const char> r = vg + (int64_t)(base + 16 * t + 4 * quad + i) * (D / 2) + (DL / 2) * c;
-          if constexpr (D == 128) w.v[t][i][0] = *reinterpret_cast<gptr<const uint32_t>>(r);
-          else w.v[t][i][0] = *reinterpret_cast<gptr<const uint16_t>>(r);
-        }
-      } else {
-        constexpr int B = CT == kCacheF32 ? 4 : 2;
-        const gptr<const char> p = kg + key_of(min(base + 16 * t + c, n - 1)) * k_row + 16 * quad;
-#pragma unroll
-        for (int s = 0; s < NK; ++s) w.k[t][s] = load16(p + 64 * s);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const gptr<const char> r =
-              vg + key_of(min(base + 16 * t + 4 * quad + i, n - 1)) * v_row + DL * B * c;
-          if constexpr (VW >= 4) {
-#pragma unroll
-            for (int u = 0; u < VW / 4; ++u) {
-              const uint4 h = load16(r + 16 * u);
-              w.v[t][i][4 * u] = h.x, w.v[t][i][4 * u + 1] = h.y;
-              w.v[t][i][4 * u + 2] = h.z, w.v[t][i][4 * u + 3] = h.w;
-            }
-          } else {
-            const uint64_t h = *reinterpret_cast<gptr<const uint64_t>>(r);
-            w.v[t][i][0] = (uint32_t)h, w.v[t][i][VW - 1] = (uint32_t)(h >> 32);
-          }
-        }
-      }
-      if constexpr (SRC == kOverCache) {
-        if constexpr (MASKS) {
-          const int32_t *p = a.c.pos + (int64_t)bg * a.c.capacity;
-          const int s = base + 16 * t + 4 * quad;
-          w.pos[t] = make_int4(p[min(s, n - 1)], p[min(s + 1, n - 1)], p[min(s + 2, n - 1)],
-                               p[min(s + 3, n - 1)]);
-        }
-      }
-    }
-  };
-
   float m[RT], l[RT];
   f32x4 acc[RT][DL];
 #pragma unroll
@@ -443,7 +475,7 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
         for (int i = 0; i < 4; ++i) {
           if constexpr (CT == kCacheFp4) {
             const int block = D == 128 ? c >> 2 : c >> 3;
-            const float sc = fp4_scale((w.vs[t][i] >> (8 * block)) & 0xFFu);
+            const float sc = fp4_scale(__builtin_amdgcn_ubfe(w.vs[t][i], 8 * block, 8));
             const uint4 x = fp4_values(w.v[t][i][0], sc);
             u[4 * t + i][0] = x.x, u[4 * t + i][1] = x.y;
             if constexpr (DL == 8) u[4 * t + i][DL / 2 - 2] = x.z, u[4 * t + i][DL / 2 - 1] = x.w;
@@ -525,11 +557,7 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
 
   // ---- the wave's steps: each one's registers are loaded again as soon as it is done
   {
-    AttendRaw<CT, D> w[DEPTH];
     int st = st0 + wave;
-#pragma unroll
-    for (int i = 0; i < DEPTH; ++i)
-      if (st + i * NW < st1) load(st + i * NW, w[i]);
     while (st < st1) {
       bool done = false;
 #pragma unroll
@@ -543,8 +571,10 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
     }
   }
 
-  // ---- join the waves: of every lane's output, four runs of DL head dimensions
-  constexpr int OS = 4 * DL + 4;                   // padded row of one run of the four quads
+  // ---- join the waves: of every lane's output, four runs of DL head dimensions, one
+  // after the other (in one workgroup, which waits for this, all at once)
+  constexpr int RUNS = ONE ? 4 : 1;
+  constexpr int OS = 4 * DL * RUNS + 4;            // padded row of RUNS runs of the four quads
   __shared__ __align__(16) float o_s[NW][16][OS];
   __shared__ float2 ml_s[NW][RM];
   __shared__ float2 row_s[RM];                     // (reference, 1 / sum) of the joined rows
@@ -574,18 +604,22 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (rt || i) __syncthreads();
+    for (int i0 = 0; i0 < 4; i0 += RUNS) {
+      if (rt || i0) __syncthreads();
 #pragma unroll
-      for (int j = 0; j < DL; j += 4)
-        *reinterpret_cast<f32x4 *>(&o_s[wave][c][DL * quad + j]) =
-            f32x4{acc[rt][j][i], acc[rt][j + 1][i], acc[rt][j + 2][i], acc[rt][j + 3][i]};
+      for (int i = i0; i < i0 + RUNS; ++i)
+#pragma unroll
+        for (int j = 0; j < DL; j += 4)
+          *reinterpret_cast<f32x4 *>(&o_s[wave][c][DL * (4 * (i - i0) + quad) + j]) =
+              f32x4{acc[rt][j][i], acc[rt][j + 1][i], acc[rt][j + 2][i], acc[rt][j + 3][i]};
       __syncthreads();
-      // 16 rows of 4 DL values, four to a thread: value DL quad + j is head dimension
-      // DL (4 quad + i) + j
-      const int row = tid / DL, x = 4 * (tid % DL), d = DL * (4 * (x / DL) + i) + x % DL;
-      const int r = rb * RM + 16 * rt + row;
-      if (row < 16 && r < rows) {
+      // 16 rows of 4 DL RUNS values, four to a thread: value DL (4 i + quad) + j of a run is
+      // head dimension DL (4 quad + i) + j
+      for (int e = tid; e < 16 * DL * RUNS; e += NTH) {
+        const int row = e / (DL * RUNS), x = 4 * (e % (DL * RUNS)), part = x / DL;
+        const int d = DL * (4 * (part % 4) + i0 + part / 4) + x % DL;
+        const int r = rb * RM + 16 * rt + row;
+        if (r >= rows) break;
         f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
@@ -613,6 +647,7 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
     if (a.accumulate)
       for (int x = tid; x < n; x += NTH) {
         float got = 0.f;
+#pragma unroll 4
         for (int r = 0; r < rows; ++r)
           got += fast_exp2(__builtin_fmaf(logit_s[r * (int)a.logit_stride + x], a.c1, -row_s[r].x)) *
                  row_s[r].y;
