@@ -72,26 +72,30 @@ struct LoadArgs {
   const int32_t *idx, *cu;
   int64_t rows_per_b;           // source rows per sequence
   int32_t n_rows;               // per group (0: ragged)
-  int32_t batch;
   int32_t off[kMaxKvHeads + 1]; // ragged: first row of a group within its sequence
 };
 
-// Grid (blocks, 3), 256 threads.  y = 0, 1: K, V rows, a lane per 8 values, so
-// that a wave reads 1 KB (bf16) in a row; y = 2: one workgroup per group counts
-// its kept rows.  Bound by HBM: 2 D values read, a 4-bit row written.
+constexpr int kUnits = 4;           // 8-value units that a lane of a load or read takes
+
+// Grid (blocks, groups, 3), 256 threads.  z = 0, 1: the group's K, V rows, a lane per 8
+// values and kUnits of these, so that a wave reads 1 KB (bf16) in a row; all
+// positions are asked for before the rows, and rows that were not kept are not
+// read.  z = 2: the first workgroup counts the kept rows.  Bound by HBM: 2 D values
+// read, a 4-bit row written.  (A grid over the groups: 64-bit divisions of a
+// flat index took longer than the rows.)
 template <typename T, int D, bool FP4>
 __global__ __launch_bounds__(256) void cache_load_kernel(const LoadArgs a) {
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, bg = blockIdx.y;
+  const int b = bg / a.c.Hkv, g = bg - b * a.c.Hkv;
   constexpr int U = D / 8;                       // lanes per row
-  if (blockIdx.y == 2) {
-    const int bg = blockIdx.x;
-    if (bg >= a.c.groups) return;                // uniform
-    const int b = bg / a.c.Hkv, g = bg - b * a.c.Hkv;
-    const int n = a.n_rows ? a.n_rows : a.off[g + 1] - a.off[g];
-    const int32_t *id = a.idx + (int64_t)b * a.rows_per_b +
-                        (a.n_rows ? (int64_t)g * a.n_rows : (int64_t)a.off[g]);
+  const int n = a.n_rows ? a.n_rows : a.off[g + 1] - a.off[g];
+  const int64_t row0 = (int64_t)b * a.rows_per_b + (a.n_rows ? (int64_t)g * a.n_rows : (int64_t)a.off[g]);
+  const int32_t *idx = a.idx + row0;
+  if (blockIdx.z == 2) {
+    if (blockIdx.x) return;                      // uniform
     int kept = 0;
-    for (int j = tid; j < n; j += 256) kept += id[j] >= 0;
+#pragma unroll 4
+    for (int j = tid; j < n; j += 256) kept += idx[j] >= 0;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) kept += __shfl_xor(kept, o);
     __shared__ int part[4];
@@ -103,34 +107,29 @@ __global__ __launch_bounds__(256) void cache_load_kernel(const LoadArgs a) {
     }
     return;
   }
-  const int64_t unit = (int64_t)blockIdx.x * 256 + tid, row = unit / U;
-  const int u = (int)(unit % U);
-  if (row >= a.batch * a.rows_per_b) return;     // whole rows, so whole 4-lane blocks
-  const int b = (int)(row / a.rows_per_b);
-  const int r = (int)(row - b * a.rows_per_b);
-  int g, j;
-  if (a.n_rows) {
-    g = r / a.n_rows;
-    j = r - g * a.n_rows;
-  } else {
-    int lo = 0, hi = a.c.Hkv;                    // off[lo] <= r < off[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (a.off[mid] <= r) lo = mid; else hi = mid;
-    }
-    g = lo;
-    j = r - a.off[g];
+  const bool is_v = blockIdx.z == 1;
+  const gptr<const char> src = to_global(is_v ? a.v : a.k) + row0 * (D * (int64_t)sizeof(T));
+  const int u = tid % U, j0 = (int)blockIdx.x * (256 / U * kUnits) + tid / U;
+  int32_t position[kUnits];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    const int j = j0 + 256 / U * i;
+    position[i] = j < n ? idx[j] : -1;
   }
-  const int32_t position = a.idx[row];
-  uint4 raw[sizeof(T) / 2];
-  const bool is_v = blockIdx.y == 1;
-  load8<T>(to_global(is_v ? a.v : a.k) + unit * (8 * (int64_t)sizeof(T)), raw);
-  if (position < 0) return;                      // the four lanes of a block agree
-  const int64_t slot = ((int64_t)b * a.c.Hkv + g) * a.c.capacity + j;
-  store8<T, D, FP4>(is_v ? a.c.v : a.c.k, is_v ? a.c.v_scale : a.c.k_scale, slot, u, raw);
-  if (!is_v && u == 0) {
-    a.c.pos[slot] = position;
-    a.c.weight[slot] = 0.f;
+  uint4 raw[kUnits][sizeof(T) / 2];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i)
+    if (position[i] >= 0)
+      load8<T>(src + ((int64_t)(j0 + 256 / U * i) * U + u) * (8 * (int64_t)sizeof(T)), raw[i]);
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    if (position[i] < 0) continue;               // the four lanes of a block agree
+    const int64_t slot = (int64_t)bg * a.c.capacity + j0 + 256 / U * i;
+    store8<T, D, FP4>(is_v ? a.c.v : a.c.k, is_v ? a.c.v_scale : a.c.k_scale, slot, u, raw[i]);
+    if (!is_v && u == 0) {
+      a.c.pos[slot] = position[i];
+      a.c.weight[slot] = 0.f;
+    }
   }
 }
 
@@ -184,35 +183,48 @@ __global__ __launch_bounds__(256) void cache_len_kernel(const CacheView c, int n
   c.seen[bg] = (int32_t)((uint32_t)c.seen[bg] + (uint32_t)n_new);
 }
 
-// Grid (blocks, 2), 256 threads: 8 values of a K (y = 0) or V row per lane.
+// Grid (blocks, groups, 2), 256 threads: K (z = 0) or V, a lane per 8 values and kUnits
+// of these.
 template <typename T, int D, bool FP4>
 __global__ __launch_bounds__(256) void cache_read_kernel(const CacheView c, char *k_out,
                                                          char *v_out) {
   constexpr int U = D / 8;
-  const bool is_v = blockIdx.y == 1;
-  const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x, slot = unit / U;
-  if (slot >= (int64_t)c.groups * c.capacity) return;
-  const int u = (int)(unit % U), bg = (int)(slot / c.capacity);
-  uint4 raw[sizeof(T) / 2] = {};
-  if ((int)(slot - (int64_t)bg * c.capacity) < live_slots(c, bg)) {
-    const char *rows = is_v ? c.v : c.k;
+  const bool is_v = blockIdx.z == 1;
+  const int bg = blockIdx.y, live = live_slots(c, bg), u = threadIdx.x % U;
+  const int j0 = (int)blockIdx.x * (256 / U * kUnits) + (int)threadIdx.x / U;
+  const char *rows = is_v ? c.v : c.k;
+  const uint8_t *scales = is_v ? c.v_scale : c.k_scale;
+  const int64_t slot0 = (int64_t)bg * c.capacity + j0;
+  uint4 raw[kUnits][sizeof(T) / 2] = {};
+  uint32_t code[kUnits] = {}, byte[kUnits] = {};
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    const int64_t slot = slot0 + 256 / U * i;
+    if (j0 + 256 / U * i >= live) continue;
     if constexpr (FP4) {
-      const uint8_t *scales = is_v ? c.v_scale : c.k_scale;
-      const uint4 w = fp4_values(reinterpret_cast<const uint32_t *>(rows)[unit],
-                                 fp4_scale(scales[slot * (D / 32) + (u >> 2)]));
-      if constexpr (sizeof(T) == 2) {
-        raw[0] = w;
-      } else {
-        raw[0] = make_uint4(w.x << 16, w.x & 0xFFFF0000u, w.y << 16, w.y & 0xFFFF0000u);
-        raw[sizeof(T) / 2 - 1] = make_uint4(w.z << 16, w.z & 0xFFFF0000u, w.w << 16, w.w & 0xFFFF0000u);
-      }
+      code[i] = to_global(reinterpret_cast<const uint32_t *>(rows))[slot * U + u];
+      byte[i] = to_global(scales)[slot * (D / 32) + (u >> 2)];
     } else {
-      load8<T>(to_global(rows) + unit * (8 * (int64_t)sizeof(T)), raw);
+      load8<T>(to_global(rows) + (slot * U + u) * (8 * (int64_t)sizeof(T)), raw[i]);
     }
   }
-  const gptr<char> to = to_global(is_v ? v_out : k_out) + unit * (8 * (int64_t)sizeof(T));
-  store16(to, raw[0]);
-  if constexpr (sizeof(T) == 4) store16(to + 16, raw[1]);
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    const int64_t slot = slot0 + 256 / U * i;
+    if (j0 + 256 / U * i >= c.capacity) break;
+    if constexpr (FP4) {
+      const uint4 w = fp4_values(code[i], fp4_scale(byte[i]));
+      if constexpr (sizeof(T) == 2) {
+        raw[i][0] = w;
+      } else {
+        raw[i][0] = make_uint4(w.x << 16, w.x & 0xFFFF0000u, w.y << 16, w.y & 0xFFFF0000u);
+        raw[i][sizeof(T) / 2 - 1] = make_uint4(w.z << 16, w.z & 0xFFFF0000u, w.w << 16, w.w & 0xFFFF0000u);
+      }
+    }
+    const gptr<char> to = to_global(is_v ? v_out : k_out) + (slot * U + u) * (8 * (int64_t)sizeof(T));
+    store16(to, raw[i][0]);
+    if constexpr (sizeof(T) == 4) store16(to + 16, raw[i][sizeof(T) / 2 - 1]);
+  }
 }
 
 // ---------------------------------------------------------------- eviction
@@ -630,14 +642,12 @@ int compresskv_cache_load(const ckv_cache *c, int32_t dtype, int32_t n_rows, con
   a.idx = idx;
   a.cu = cu_seqlens;
   a.rows_per_b = per_b;
-  a.batch = c->batch;
-  const int64_t blocks = std::max<int64_t>(
-      a.c.groups, ((int64_t)c->batch * per_b * (c->head_dim / 8) + 255) / 256);
-  if (blocks > INT32_MAX / 256)
-    return fail(CKV_UNSUPPORTED, "batch * rows is too large for one launch");
+  const int rows_per_block = 256 / (c->head_dim / 8) * ckv::kUnits;
+  int most = n_rows;
+  if (group_rows_host) most = *std::max_element(group_rows_host, group_rows_host + c->n_kv_heads);
+  const dim3 grid((most + rows_per_block - 1) / rows_per_block, a.c.groups, 3);
   with_rows(c, dtype, [&]<typename T, int D, bool FP4>() {
-    hipLaunchKernelGGL((ckv::cache_load_kernel<T, D, FP4>), dim3((unsigned)blocks, 3), dim3(256), 0,
-                       (hipStream_t)stream, a);
+    hipLaunchKernelGGL((ckv::cache_load_kernel<T, D, FP4>), grid, dim3(256), 0, (hipStream_t)stream, a);
   });
   return launched("cache load");
 }
@@ -695,13 +705,11 @@ int compresskv_cache_read(const ckv_cache *c, int32_t dtype, void *k_out, void *
   if ((st = check_pointer(k_out, "k_out", 16))) return st;
   if ((st = check_pointer(v_out, "v_out", 16))) return st;
   const ckv::CacheView v = cache_view(c);
-  const int64_t blocks = ((int64_t)v.groups * c->capacity * (c->head_dim / 8) + 255) / 256;
-  if (blocks > INT32_MAX / 256)
-    return fail(CKV_UNSUPPORTED, "batch * capacity is too large for one launch");
+  const int rows_per_block = 256 / (c->head_dim / 8) * ckv::kUnits;
+  const dim3 grid((c->capacity + rows_per_block - 1) / rows_per_block, v.groups, 2);
   with_rows(c, dtype, [&]<typename T, int D, bool FP4>() {
-    hipLaunchKernelGGL((ckv::cache_read_kernel<T, D, FP4>), dim3((unsigned)blocks, 2), dim3(256), 0,
-                       (hipStream_t)stream, v, static_cast<char *>(k_out),
-                       static_cast<char *>(v_out));
+    hipLaunchKernelGGL((ckv::cache_read_kernel<T, D, FP4>), grid, dim3(256), 0, (hipStream_t)stream, v,
+                       static_cast<char *>(k_out), static_cast<char *>(v_out));
   });
   return launched("cache read");
 }
