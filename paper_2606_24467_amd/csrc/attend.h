@@ -48,7 +48,7 @@ void launch_attend(const AttendArgs &a, AttendSource source, CacheType type, boo
 // that many 16-row tiles.
 constexpr int kPromptRows = 128;
 constexpr int64_t kPromptMaxStride = 1 << 24;   // bytes between tokens: 64 rows stay within 32 bits
-void launch_window_prompt(const AttendArgs &a, int head_dim, int max_rows, hipStream_t stream);
+void launch_window_prompt(const AttendArgs &a, int head_dim, int blocks, int max_rows, hipStream_t stream);
 
 // Joins the splits' outputs, and adds to the weights if a.accumulate.
 void launch_attend_join(AttendArgs a, AttendSource source, bool f32, int head_dim,

@@ -333,7 +333,7 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
   __shared__ uint64_t list_s[kEvictList];   // key << 32 | ~slot: the first ones go first
   __shared__ int freed_s[kEvictList];       // of each, its slot if it is freed below the budget
   __shared__ uint8_t tail_gone_s[kFusedMoves];
-  __shared__ uint32_t keys_s[LKEYS ? LKEYS : 1];
+  __shared__ __align__(16) uint32_t keys_s[LKEYS ? LKEYS : 1];   // of the slots
   __shared__ int listed_s, moves_s;
   const int tid = threadIdx.x, lane = tid & 63, bg = blockIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -353,16 +353,43 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
     const uint32_t k = evict_key(weight[s], pos[s], a.n_sinks, recent_from);
     return slot < n ? k : 0xFFFFFFFFu;
   };
+  // f(slot, keys of slot .. slot + 3) for all of the wave's slots: 16-byte loads of four
+  // slots a lane (to 4 bytes aligned, as a group begins anywhere), several under way
+  auto each_four = [&](auto &&f) {
+    typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+    typedef int32_t i4 __attribute__((ext_vector_type(4), aligned(4)));
+    const int begin = wave * 64 * nj;
+    const int whole = min(max(a.c.capacity - begin, 0) / 256, nj / 4);
+    int slot = begin + 4 * lane;
+#pragma unroll 4
+    for (int i = 0; i < whole; ++i, slot += 256) {
+      const f4 w = *reinterpret_cast<const f4 *>(weight + slot);
+      const i4 p = *reinterpret_cast<const i4 *>(pos + slot);
+      uint32_t k[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        k[e] = evict_key(w[e], p[e], a.n_sinks, recent_from);
+        k[e] = slot + e < n ? k[e] : 0xFFFFFFFFu;
+      }
+      f(slot, k);
+    }
+#pragma unroll 1
+    for (int i = whole; i < nj / 4; ++i, slot += 256) {      // past the capacity
+      uint32_t k[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[e] = read_key(slot + e);
+      f(slot, k);
+    }
+  };
   const int drop = n - a.budget;
   int moves = 0;
   if (drop == 1) {
     uint64_t least = ~0ull;
-#pragma unroll 8
-    for (int j = 0; j < nj; ++j) {
-      const int slot = first + 64 * j;
-      const uint64_t k = (uint64_t)read_key(slot) << 32 | (uint32_t)~slot;
-      if (slot < n) least = min(least, k);
-    }
+    each_four([&](int slot, const uint32_t (&k)[4]) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (slot + e < n) least = min(least, (uint64_t)k[e] << 32 | (uint32_t)~(slot + e));
+    });
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) least = min(least, (uint64_t)__shfl_xor((unsigned long long)least, o));
     if (lane == 0) least_s[wave] = least;
@@ -384,16 +411,15 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
     return;
   }
   uint32_t least = 0xFFFFFFFFu;
-#pragma unroll 8
-  for (int j = 0; j < nj; ++j) {
-    const uint32_t k = read_key(first + 64 * j);
-    least = min(least, k);
-    if (LKEYS) keys_s[tid + NT * j] = k;         // read by this thread alone
-  }
+  each_four([&](int slot, const uint32_t (&k)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) least = min(least, k[e]);
+    if (LKEYS) *reinterpret_cast<uint4 *>(&keys_s[slot]) = make_uint4(k[0], k[1], k[2], k[3]);   // for this wave
+  });
   // keys j .. j + 3, together
   auto keys_at = [&](int j, uint32_t (&k)[4]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) k[e] = LKEYS ? keys_s[tid + NT * (j + e)] : read_key(first + 64 * (j + e));
+    for (int e = 0; e < 4; ++e) k[e] = LKEYS ? keys_s[first + 64 * (j + e)] : read_key(first + 64 * (j + e));
   };
   if (tid < 128) reinterpret_cast<int *>(count_s)[tid] = 0;
   if (tid == 0) listed_s = 0;

@@ -20,6 +20,7 @@ constexpr int32_t kMaxTokens = 1 << 30;
 struct WindowPlan {
   ckv::AttendArgs a;
   int64_t max_rows;             // query rows of one (sequence, group)
+  int64_t blocks;               // row blocks of all, where the kernel for many rows takes them
   bool prompt;                  // the kernel for many rows
   size_t ml_bytes, o_bytes;
   size_t total() const { return ml_bytes + o_bytes; }
@@ -80,13 +81,14 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
   a.c.groups = p->batch * p->n_kv_heads;
   a.Hkv = p->n_kv_heads;
   a.G = p->n_q_heads / p->n_kv_heads;
-  pl.max_rows = 0;
+  pl.max_rows = pl.blocks = 0;
   int64_t keys = 0;              // that a row block may read, at most
   for (int b = 0; b < p->batch; ++b) {
     const int64_t lq = p->cu_q_host[b + 1] - p->cu_q_host[b];
     const int64_t lk = p->cu_k_host[b + 1] - p->cu_k_host[b];
     if (lq == 0) continue;
     pl.max_rows = std::max(pl.max_rows, lq * a.G);
+    pl.blocks += (lq * a.G + ckv::kPromptRows - 1) / ckv::kPromptRows * a.Hkv;
     const int64_t span = std::min<int64_t>(lq, ckv::kPromptRows / a.G + 1);   // tokens of a block
     keys = std::max(keys, std::min<int64_t>(lk, (int64_t)p->window + p->n_sinks + span - 1));
   }
@@ -100,7 +102,7 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
   if (blocks > 1 << 23) return fail(CKV_UNSUPPORTED, "too many query rows for one launch");
   a.masks = pl.max_rows > a.G;   // more than one token in some row block
   a.one = !pl.prompt && ckv::attend_in_one(pl.max_rows, keys, false);
-  a.splits = pl.prompt ? prompt_splits(blocks, keys)
+  a.splits = pl.prompt ? prompt_splits(pl.blocks, keys)
              : a.one   ? 1
                        : ckv::attend_splits(blocks, keys);
   a.window = std::min(p->window, kMaxTokens);   // positions plus or minus either stay in 32 bits
@@ -158,7 +160,7 @@ int compresskv_window_attention(const ckv_window_problem *p, const void *q, cons
   a.part_o = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.ml_bytes);
   const bool f32 = p->dtype == CKV_F32;
   if (pl.prompt)
-    ckv::launch_window_prompt(a, p->head_dim, (int)pl.max_rows, (hipStream_t)stream);
+    ckv::launch_window_prompt(a, p->head_dim, (int)pl.blocks, (int)pl.max_rows, (hipStream_t)stream);
   else
     ckv::launch_attend(a, ckv::kOverWindow, f32 ? ckv::kCacheF32 : ckv::kCacheBf16, f32, p->head_dim,
                        (int)pl.max_rows, (hipStream_t)stream);

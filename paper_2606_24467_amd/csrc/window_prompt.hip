@@ -50,7 +50,8 @@ __device__ __forceinline__ void add_unbounded32(f32x16 &acc, bf16x8 &v, bf16x8 s
 }
 
 template <int D>
-__global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(const AttendArgs a, int run) {
+__global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(const AttendArgs a, int blocks,
+                                                                            int run) {
   constexpr int NF = D / 16, DB = D / 32;        // K fragments, blocks of 32 head dimensions
   constexpr int U = D / 8;                       // 16-byte units per row
   constexpr int LD = kPromptKeys * U / (64 * kPromptWaves);   // loads of K (of V) per wave and tile
@@ -66,18 +67,44 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 31, h = lane >> 5;
 
-  // Consecutive row blocks of a group share their keys, so runs of them go to one
-  // XCD (workgroups go round the XCDs in turn), the latest rows first; and the runs
-  // go round the XCDs, so that sequences of different lengths load them alike.
-  const int in_xcd = (int)blockIdx.x >> 3, runs = (a.row_blocks + run - 1) / run;
-  const int id = in_xcd / run * 8 + ((int)blockIdx.x & 7), bg = id / runs;
-  const int rb = a.row_blocks - 1 - ((id - bg * runs) * run + in_xcd % run);
-  if (bg >= a.c.groups || rb < 0) return;        // uniform
-  const int b = bg / a.Hkv, g = bg - b * a.Hkv;
-  const int q0 = a.cu_q[b], k0 = a.cu_k[b];
-  const int lq = a.cu_q[b + 1] - q0, lk = a.cu_k[b + 1] - k0;
+  // The row blocks that there are, sequence by sequence and group by group, are
+  // numbered without gaps.  Consecutive ones share their keys, so runs of them go to
+  // one XCD (workgroups go round the XCDs in turn) and the runs go round the XCDs, the
+  // latest rows of a group first.  Each wave finds its sequence: 64 at a time, a lane each.
+  const int in_xcd = (int)blockIdx.x >> 3;
+  int id = (in_xcd / run * 8 + ((int)blockIdx.x & 7)) * run + in_xcd % run;
+  if (id >= blocks) return;                      // uniform
+  const int batch = a.c.groups / a.Hkv;
+  int b = -1, nb = 0, q0 = 0, k0 = 0, lq = 0, lk = 0;
+  for (int b0 = 0; b0 < batch; b0 += 64) {
+    const int at = min(b0 + lane, batch - 1);
+    const int q_at = a.cu_q[at], q_to = a.cu_q[at + 1], k_at = a.cu_k[at], k_to = a.cu_k[at + 1];
+    const int64_t of_group = ((int64_t)(q_to - q_at) * a.G + kPromptRows - 1) / kPromptRows;
+    const int mine = b0 + lane < batch ? (int)max((int64_t)0, min(of_group, (int64_t)a.row_blocks)) : 0;
+    int upto = mine * a.Hkv;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int before = __shfl_up(upto, o);
+      upto += lane >= o ? before : 0;
+    }
+    const uint64_t beyond = __ballot(upto > id);
+    if (beyond == 0) {
+      id -= __builtin_amdgcn_readlane(upto, 63);
+      continue;
+    }
+    const int src = __builtin_ctzll(beyond);
+    b = b0 + src;
+    nb = __builtin_amdgcn_readlane(mine, src);
+    id -= __builtin_amdgcn_readlane(upto, src) - nb * a.Hkv;
+    q0 = __builtin_amdgcn_readlane(q_at, src);
+    k0 = __builtin_amdgcn_readlane(k_at, src);
+    lq = __builtin_amdgcn_readlane(q_to, src) - q0;
+    lk = __builtin_amdgcn_readlane(k_to, src) - k0;
+    break;
+  }
+  if (b < 0) return;                             // uniform
+  const int g = id / nb, rb = nb - 1 - (id - g * nb), bg = b * a.Hkv + g;
   const int rows = lq * a.G, r0 = rb * kPromptRows;
-  if (r0 >= rows) return;                        // uniform
   const int t0 = lk - lq;                        // position of query token 0
   const int t_first = t0 + r0 / a.G, t_last = t0 + (min(rows, r0 + kPromptRows) - 1) / a.G;
   // the keys that any row sees, counted from 0 ("virtual"): the sinks outside the
@@ -196,6 +223,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   auto work = [&]<bool UNBOUNDED, int BUF>(int tile) {
     const char *kt = BUF ? odd_s : even_s, *vt = kt + KB;
     f32x16 s[2] = {f32x16{}, f32x16{}};
+    __builtin_amdgcn_s_setprio(1);               // the logits' products before another wave's softmax
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -211,16 +239,22 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
       }
       __builtin_amdgcn_sched_group_barrier(0x008, NF, 0);
     }
+    __builtin_amdgcn_s_setprio(0);
     if (UNBOUNDED || !within(tile, w_from, w_to)) {
+      // the keys of the tile that this lane's row sees, a bit each; two instructions a logit
       const int from = tile * kPromptKeys, last = last_x - from, first = first_x - from;
       const int sink = min(a.sinks - 4 * h - from, last + 1);
+      auto below = [](int x) { return x >= 64 ? ~0ull : x <= 0 ? 0ull : ~0ull >> (64 - x); };
+      const uint64_t seen = (below(last + 1) & ~below(first)) | below(sink);
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t word = (uint32_t)(seen >> (32 * k));
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const int x = 32 * k + 8 * (i >> 2) + (i & 3);
-          s[k][i] = (x >= first && x <= last) || x < sink ? s[k][i] : -INFINITY;
+          const uint32_t all = __builtin_amdgcn_sbfe(word, 8 * (i >> 2) + (i & 3), 1);
+          s[k][i] = __uint_as_float((__float_as_uint(s[k][i]) & all) | (0xFF800000u & ~all));
         }
+      }
     }
     // (the maximum that returns a NaN needs no quieting of its operands)
     float top = __builtin_elementwise_maximum(s[0][0], s[1][0]);
@@ -371,16 +405,15 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   }
 }
 
-void launch_window_prompt(const AttendArgs &a, int head_dim, int max_rows, hipStream_t stream) {
+void launch_window_prompt(const AttendArgs &a, int head_dim, int blocks, int max_rows, hipStream_t stream) {
   // 32 row blocks (half of what an XCD holds at a time) in a run, fewer where that
-  // would leave an XCD with less than about four runs
-  const int run = (int)std::clamp<int64_t>((int64_t)a.row_blocks * a.c.groups / 32, 1, 32);
-  const int64_t runs = (int64_t)((a.row_blocks + run - 1) / run) * a.c.groups;
-  const dim3 grid((unsigned)((runs + 7) / 8 * 8 * run), a.splits);
+  // would leave an XCD with less than about 16 runs
+  const int run = std::clamp(blocks / 128, 1, 32);
+  const dim3 grid((unsigned)(((int64_t)blocks + 8 * run - 1) / (8 * run) * (8 * run)), a.splits);
   if (head_dim == 64)
-    hipLaunchKernelGGL((window_prompt_kernel<64>), grid, dim3(64 * kPromptWaves), 0, stream, a, run);
+    hipLaunchKernelGGL((window_prompt_kernel<64>), grid, dim3(64 * kPromptWaves), 0, stream, a, blocks, run);
   else
-    hipLaunchKernelGGL((window_prompt_kernel<128>), grid, dim3(64 * kPromptWaves), 0, stream, a, run);
+    hipLaunchKernelGGL((window_prompt_kernel<128>), grid, dim3(64 * kPromptWaves), 0, stream, a, blocks, run);
   launch_attend_join(a, kOverWindow, false, head_dim, max_rows, stream);
 }
 

@@ -127,3 +127,17 @@ def test_a_long_sequence_in_pieces(gpu):
         # both are off by at most half a step of bf16 in the output and in each probability
         size = np.abs(H.values(v[:n])).max()
         assert np.abs(got - whole[a:e]).max() <= 4 * 2.0 ** -8 * size
+
+
+def test_window_attention_of_many_sequences(gpu):
+    """More sequences than a wave looks at together, some of them empty, in the kernel for many rows."""
+    rng = np.random.default_rng(11)
+    spans = [(int(x), int(x + y)) for x, y in zip(rng.integers(0, 40, 150), rng.integers(0, 30, 150))]
+    spans[0] = spans[64] = spans[149] = (0, 7)
+    spans[63], spans[128] = (33, 33), (70, 90)
+    q, k, v, cu_q, cu_k = _inputs(spans, 4, 1, 64, BF16, gpu, 12)
+    p = C.WindowProblem(q, k, v, cu_q, cu_k, window=20, n_sinks=2)
+    out = torch.full_like(q, 7.0)
+    C.window_attention(p, q, k, v, out=out)
+    _check(q, k, v, spans, 20, 2, out)
+    assert (out[sum(s[0] for s in spans):] == 7.0).all()
