@@ -141,3 +141,16 @@ def test_window_attention_of_many_sequences(gpu):
     C.window_attention(p, q, k, v, out=out)
     _check(q, k, v, spans, 20, 2, out)
     assert (out[sum(s[0] for s in spans):] == 7.0).all()
+
+
+def test_window_attention_of_thousands_of_sequences(gpu):
+    rng = np.random.default_rng(13)
+    spans = [(0, 0)] * 4500
+    for s in rng.choice(4500, 120, replace=False):
+        spans[s] = (int(rng.integers(1, 40)),) * 2
+    spans[4499] = (50, 61)
+    q, k, v, cu_q, cu_k = _inputs(spans, 2, 1, 64, BF16, gpu, 14)
+    p = C.WindowProblem(q, k, v, cu_q, cu_k, window=20, n_sinks=2)
+    out = C.window_attention(p, q, k, v)
+    keep = [s for s in spans if s[0]]
+    _check(q, k, v, keep, 20, 2, out)
