@@ -360,21 +360,30 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
     typedef int32_t i4 __attribute__((ext_vector_type(4), aligned(4)));
     const int begin = wave * 64 * nj;
     const int whole = min(max(a.c.capacity - begin, 0) / 256, nj / 4);
-    int slot = begin + 4 * lane;
-#pragma unroll 4
-    for (int i = 0; i < whole; ++i, slot += 256) {
-      const f4 w = *reinterpret_cast<const f4 *>(weight + slot);
-      const i4 p = *reinterpret_cast<const i4 *>(pos + slot);
-      uint32_t k[4];
+    for (int i = 0; i < whole; i += 4) {
+      f4 w[4];
+      i4 p[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        k[e] = evict_key(w[e], p[e], a.n_sinks, recent_from);
-        k[e] = slot + e < n ? k[e] : 0xFFFFFFFFu;
+      for (int u = 0; u < 4; ++u) {
+        const int slot = begin + 4 * lane + 256 * min(i + u, whole - 1);
+        w[u] = *reinterpret_cast<const f4 *>(weight + slot);
+        p[u] = *reinterpret_cast<const i4 *>(pos + slot);
       }
-      f(slot, k);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (i + u >= whole) break;               // uniform
+        const int slot = begin + 4 * lane + 256 * (i + u);
+        uint32_t k[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          k[e] = evict_key(w[u][e], p[u][e], a.n_sinks, recent_from);
+          k[e] = slot + e < n ? k[e] : 0xFFFFFFFFu;
+        }
+        f(slot, k);
+      }
     }
-#pragma unroll 1
-    for (int i = whole; i < nj / 4; ++i, slot += 256) {      // past the capacity
+    for (int i = whole; i < nj / 4; ++i) {       // past the capacity
+      const int slot = begin + 4 * lane + 256 * i;
       uint32_t k[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) k[e] = read_key(slot + e);
@@ -421,6 +430,22 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) k[e] = LKEYS ? keys_s[first + 64 * (j + e)] : read_key(first + 64 * (j + e));
   };
+  // f(slot, key) for all of the wave's slots, in any order
+  auto each_key = [&](auto &&f) {
+    if constexpr (LKEYS > 0) {
+      for (int j = 0; j < nj; j += 4) {
+        uint32_t k[4];
+        keys_at(j, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(first + 64 * (j + e), k[e]);
+      }
+    } else {
+      each_four([&](int slot, const uint32_t (&k)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f(slot + e, k[e]);
+      });
+    }
+  };
   if (tid < 128) reinterpret_cast<int *>(count_s)[tid] = 0;
   if (tid == 0) listed_s = 0;
   __syncthreads();
@@ -437,16 +462,12 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
       bound = search_key<7>(count_least, count_s[0], drop, lane, less) + (1u << 18);
       if (bound == 0u) bound = 0xFFFFFFFFu;
     }
-    for (int j = 0; j < nj; j += 4) {
-      uint32_t k[4];
-      keys_at(j, k);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (k[e] < bound) {
-          const int i = atomicAdd(&listed_s, 1);
-          if (i < kEvictList) list_s[i] = (uint64_t)k[e] << 32 | (uint32_t)~(first + 64 * (j + e));
-        }
-    }
+    each_key([&](int slot, uint32_t k) {
+      if (k < bound) {
+        const int i = atomicAdd(&listed_s, 1);
+        if (i < kEvictList) list_s[i] = (uint64_t)k << 32 | (uint32_t)~slot;
+      }
+    });
     if (tid < kFusedMoves) tail_gone_s[tid] = 0;
     __syncthreads();
     const int listed = listed_s;
@@ -492,26 +513,16 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
     }
   }
   auto count_all = [&](uint32_t t1, uint32_t t2, uint32_t t3, int (&c)[3]) {
-    for (int j = 0; j < nj; j += 4) {
-      uint32_t k[4];
-      keys_at(j, k);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        c[0] += __popcll(__ballot(k[e] < t1));
-        c[1] += __popcll(__ballot(k[e] < t2));
-        c[2] += __popcll(__ballot(k[e] < t3));
-      }
-    }
+    each_key([&](int, uint32_t k) {
+      c[0] += __popcll(__ballot(k < t1));
+      c[1] += __popcll(__ballot(k < t2));
+      c[2] += __popcll(__ballot(k < t3));
+    });
   };
   t = search_key<16>(count_all, count_s[1], drop, lane, less);
   // keys below t go, and the highest slots of those equal to it
   int equal = 0;
-  for (int j = 0; j < nj; j += 4) {
-    uint32_t k[4];
-    keys_at(j, k);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) equal += __popcll(__ballot(k[e] == t && first + 64 * (j + e) < n));
-  }
+  each_key([&](int slot, uint32_t k) { equal += __popcll(__ballot(k == t && slot < n)); });
   int all_equal;
   const int equal_before = wave_prefix<NW>(equal, wave, lane, sums, all_equal);
   const int keep_equal = all_equal - (drop - less);
