@@ -151,7 +151,9 @@ typedef struct ckv_window_problem {
   float scale;          /* softmax scale; <= 0 selects 1/sqrt(head_dim) */
   const int32_t *cu_q, *cu_q_host; /* device and host [batch+1]: query tokens, cu[0] = 0 */
   const int32_t *cu_k, *cu_k_host; /* the same for the keys; non-decreasing both,
-                                      at most 2^30 tokens */
+                                      at most 2^30 tokens.  The launch is laid out
+                                      for the host's values: the device's are the same
+                                      whenever the call, or a graph of it, runs */
   int64_t q_stride_tok, q_stride_head; /* elements, multiples of 16 bytes, >= D */
   int64_t k_stride_tok, k_stride_head;
   int64_t v_stride_tok, v_stride_head;
@@ -168,9 +170,9 @@ size_t compresskv_window_attention_workspace_bytes(const ckv_window_problem *p);
  * q [Tq][Hq][D], k, v [Tk][Hkv][D] packed, with the problem's strides; out
  * [Tq][Hq][D] dense; all 16-byte aligned.  Rows of out past the last sequence
  * are not written.  Sums and softmax are held in fp32; K and V of a key that a
- * query does not see do not reach it, whatever they hold.
- * ws: >= compresskv_window_attention_workspace_bytes() ,
- * 256-byte aligned.
+ * query does not see do not reach it, whatever they hold.  Without any query
+ * nothing is done, and q and out may be NULL; without any key k and v may be.
+ * ws: >= compresskv_window_attention_workspace_bytes(), 256-byte aligned.
  */
 int compresskv_window_attention(const ckv_window_problem *p, const void *q, const void *k,
                                 const void *v, void *out, void *ws, size_t ws_bytes, void *stream);

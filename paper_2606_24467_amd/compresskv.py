@@ -664,6 +664,23 @@ def _enter(device: torch.device, stream):
     return torch.cuda.stream(stream), stream.cuda_stream
 
 
+def _used_on(stream, device: torch.device, *tensors) -> None:
+    """Tensors that a call on a stream of the caller's choice reads or writes: their memory is
+    not given out again before that stream is done with them."""
+    if stream is None:
+        return
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    for t in tensors:
+        if t is not None and t.numel():
+            t.record_stream(stream)
+
+
+def _check_ws(ws, device: torch.device) -> None:
+    if ws is not None and (ws.device != device or not ws.is_contiguous()):
+        raise ValueError(f"ws must be contiguous and on {device}")
+
+
 def _check_tensor(t, name: str, shape, dtype, device) -> None:
     if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)} (got {t.dtype} {tuple(t.shape)})")
@@ -746,6 +763,10 @@ class Cache:
         return cls(*rows, *scales, torch.full(shape, -1, dtype=torch.int32, device=device),
                    new((), torch.float32), *counts)
 
+    def _tensors(self):
+        return (self.k, self.v, self.k_scale, self.v_scale, self.pos, self.weight, self.length,
+                self.seen)
+
     def load(self, k_rows, v_rows, idx, cu_seqlens, group_budgets=None, stream=None) -> None:
         """Kept rows of compress_layer (k_out, v_out [batch, Hkv, n, D], idx [batch, Hkv, n]),
         or with group_budgets of compress_layer_heads ([batch, total, D], [batch, total])."""
@@ -772,6 +793,7 @@ class Cache:
             _check("compresskv_cache_load", lib().compresskv_cache_load(
                 self._ref, dtype, n, _ptr(k_rows), _ptr(v_rows), _ptr(idx), _ptr(gb),
                 _ptr(cu_seqlens), handle))
+        _used_on(stream, self.device, k_rows, v_rows, idx, cu_seqlens, *self._tensors())
 
     def append(self, k_new, v_new, stream=None) -> None:
         """New tokens' rows [batch, n, Hkv, D], D contiguous."""
@@ -791,6 +813,7 @@ class Cache:
             _check("compresskv_cache_append", lib().compresskv_cache_append(
                 self._ref, _row_dtype(dtype), shape[1], k_new.data_ptr(), _I64x3(*ks[:3]),
                 v_new.data_ptr(), _I64x3(*vs[:3]), handle))
+        _used_on(stream, self.device, k_new, v_new, *self._tensors())
 
     def read(self, dtype: torch.dtype | None = None, stream=None):
         """(k, v) [batch, Hkv, capacity, D] as values, zeros past the live slots."""
@@ -804,6 +827,7 @@ class Cache:
             v = torch.empty(shape, dtype=dtype, device=self.device)
             _check("compresskv_cache_read", lib().compresskv_cache_read(
                 self._ref, code, k.data_ptr(), v.data_ptr(), handle))
+        _used_on(stream, self.device, *self._tensors())
         return k, v
 
     def attend(self, q, *, scale: float | None = None, accumulate: bool = False, out=None,
@@ -815,6 +839,7 @@ class Cache:
         _check_tensor(q, "q", q.shape, q.dtype, self.device)
         if out is not None:
             _check_tensor(out, "out", q.shape, q.dtype, self.device)
+        _check_ws(ws, self.device)
         key = (q.shape[1], q.shape[2], q.dtype, bool(accumulate), scale)
         known = self._attends.get(key)
         if known is None:
@@ -835,11 +860,13 @@ class Cache:
             _check("compresskv_cache_attend", lib().compresskv_cache_attend(
                 self._ref, known[1], q.data_ptr(), out.data_ptr(), ws.data_ptr(),
                 ws.numel() * ws.element_size(), handle))
+        _used_on(stream, self.device, q, out, ws, *self._tensors())
         return out
 
     def evict(self, budget: int, *, n_sinks: int = 0, n_recent: int = 0, ws=None,
               stream=None) -> None:
         """Drops the slots of least weight of every group with more than `budget`."""
+        _check_ws(ws, self.device)
         n = self._evict_bytes.get(budget)
         if n is None:
             n = lib().compresskv_cache_evict_workspace_bytes(self._ref, int(budget))
@@ -853,6 +880,7 @@ class Cache:
             _check("compresskv_cache_evict", lib().compresskv_cache_evict(
                 self._ref, int(budget), int(n_sinks), int(n_recent), ws.data_ptr(),
                 ws.numel() * ws.element_size(), handle))
+        _used_on(stream, self.device, ws, *self._tensors())
 
 
 class WindowProblem:
@@ -915,6 +943,7 @@ def window_attention(p: WindowProblem, q, k, v, *, out=None, ws=None, stream=Non
     _check_on_gpu(p.device)
     if out is not None:
         _check_tensor(out, "out", q.shape, q.dtype, p.device)
+    _check_ws(ws, p.device)
     ctx, handle = _enter(p.device, stream)
     with ctx:
         if out is None:
@@ -924,4 +953,5 @@ def window_attention(p: WindowProblem, q, k, v, *, out=None, ws=None, stream=Non
         _check("compresskv_window_attention", lib().compresskv_window_attention(
             p._ref, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), ws.data_ptr(),
             ws.numel() * ws.element_size(), handle))
+    _used_on(stream, p.device, q, k, v, out, ws, p.cu_q, p.cu_k)
     return out

@@ -136,9 +136,11 @@ int compresskv_window_attention(const ckv_window_problem *p, const void *q, cons
   WindowPlan pl;
   int st;
   if ((st = plan_window(p, pl))) return st;
-  const void *ptrs[] = {q, k, v, out};
-  const char *names[] = {"q", "k", "v", "out"};
-  for (int i = 0; i < 4; ++i) {
+  if (pl.max_rows == 0) return ok();   // no query anywhere
+  const void *ptrs[] = {q, out, k, v};
+  const char *names[] = {"q", "out", "k", "v"};
+  const int needed = p->cu_k_host[p->batch] > 0 ? 4 : 2;   // without keys, k and v are not read
+  for (int i = 0; i < needed; ++i) {
     if (!ptrs[i]) return fail(CKV_INVALID_ARGUMENT, "%s is NULL", names[i]);
     if (!ckv_api::aligned(ptrs[i], 16))
       return fail(CKV_UNSUPPORTED, "%s must be 16-byte aligned", names[i]);
@@ -150,7 +152,6 @@ int compresskv_window_attention(const ckv_window_problem *p, const void *q, cons
       return fail(CKV_WORKSPACE_TOO_SMALL, "workspace of %zu bytes needed, %zu given", pl.total(),
                   ws_bytes);
   }
-  if (pl.max_rows == 0) return ok();   // no query anywhere
   ckv::AttendArgs &a = pl.a;
   a.q = static_cast<const char *>(q);
   a.k = static_cast<const char *>(k);

@@ -252,3 +252,11 @@ def test_binding_refuses_window_problems():
     p = C.WindowProblem(**ok)
     with pytest.raises(ValueError, match="strides"):
         C.window_attention(p, torch.zeros(9, 16, 64)[:, ::2], kv, kv)
+
+
+def test_window_without_queries_needs_no_pointers(L):
+    p, keep = _window(cu_q=(0, 0, 0))
+    assert L.compresskv_window_attention(ctypes.byref(p), None, None, None, None, None, 0, None) == 0
+    p, keep = _window(cu_k=(0, 0, 0))                     # without keys: q and out still
+    assert L.compresskv_window_attention(ctypes.byref(p), FAKE, None, None, None, FAKE, 1 << 40, None) == INV
+    assert L.compresskv_window_attention(ctypes.byref(p), None, None, None, FAKE, FAKE, 1 << 40, None) == INV
