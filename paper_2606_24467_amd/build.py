@@ -47,12 +47,16 @@ def _hipcc() -> str:
 # Per-source additions.  The two-pass scoring kernels and the attention keep
 # MFMA results in VGPRs, where the softmax arithmetic reads them (the single-pass kernel is
 # left to the default heuristics: this compiler fails on it with the option).
+# The attention kernels also go without clauses of loads.  The pass that forms them
+# (SI Form memory clauses) lost live ranges of 16-byte loads whose words are used one
+# by one: registers of V rows were given away before their last use, and the outputs
+# were wrong.  Compiled with -mllvm -verify-machineinstrs it says so ("No live subrange
+# at use"); without clauses the verifier finds nothing.
+_ATTEND = ["-mllvm", "-amdgpu-mfma-vgpr-form", "-mllvm", "-amdgpu-max-memory-clause=1"]
 EXTRA = {
     "score_kernels.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "score_layers.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "attend_fp4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "attend_bf16.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "attend_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "attend_fp4.hip": _ATTEND, "attend_bf16.hip": _ATTEND, "attend_f32.hip": _ATTEND,
 }
 
 

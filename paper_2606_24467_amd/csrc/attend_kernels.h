@@ -21,8 +21,8 @@
 // values an instruction; bf16 products then run on the 16x16x32 instruction.
 // fp32 rows run on the 16x16x4 fp32 instruction; fp32 queries over 4-bit rows
 // are split into three bf16 parts (24 bits), which loses nothing.
-// P is rounded to bf16 for bf16 queries as two parts (16 bits): the loop waits
-// for memory, so the second product costs nothing and the output is rounded
+// P goes into bf16 products, for bf16 queries, as two parts (16 bits): the loop
+// waits for memory, so the second product costs nothing and the output is rounded
 // once, at its end.
 #pragma once
 
@@ -30,6 +30,15 @@
 #include "score_common.h"
 
 namespace ckv {
+
+// A probability as two parts for bf16 products, off by 2^-16 of it at most: its upper
+// bits, and the rest rounded.  Both are positive, so that neither makes a NaN of an
+// infinite V value.
+__device__ __forceinline__ void split_probability(float p, __bf16 (&part)[2]) {
+  const uint32_t upper = __float_as_uint(p) & 0xFFFF0000u;
+  part[0] = __builtin_bit_cast(__bf16, (uint16_t)(upper >> 16));
+  part[1] = (__bf16)fmaxf(p - __uint_as_float(upper), p * 0x1p-24f);
+}
 
 // The parts that a value is split into before a bf16 product: 1 exact, 2 (16
 // bits of mantissa) or 3 (24 bits).
@@ -490,7 +499,8 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           __bf16 part[PP];
-          split_bf16<PP>(p[rt][e >> 2][e & 3], part);
+          if constexpr (PP == 2) split_probability(p[rt][e >> 2][e & 3], part);
+          else split_bf16<PP>(p[rt][e >> 2][e & 3], part);
 #pragma unroll
           for (int x = 0; x < PP; ++x) pf[rt][x][e] = part[x];
         }
