@@ -42,7 +42,6 @@ __device__ __forceinline__ void join_rows(const AttendArgs &a, int64_t slot0, in
   }
 }
 
-constexpr int64_t kOneKeys = 2048;
 constexpr int kJoinSlots = 1024;   // slots whose weights one workgroup adds to
 
 // Grid (out_blocks + weight blocks, groups), 256 threads.  The first out_blocks
@@ -168,13 +167,24 @@ int attend_row_tiles(int rows, bool three_parts) {
 }
 
 // Whether one workgroup takes all keys of a group's rows, in one launch, instead of
-// several and a join: up to kOneKeys keys, and with weights 32 KB of logits.
-bool attend_in_one(int64_t rows, int64_t keys, bool weights) {
-  return rows <= 16 && keys <= kOneKeys && (!weights || rows * ((keys + 31) / 32 * 32) <= 8192);
+// several workgroups and a join.  Where the groups alone fill half of the CUs, up to 2048
+// keys; else as many as it reads about as fast as the second launch takes, 288 KB, with 4-bit
+// rows, which are widened first, counted twice; and with weights 32 KB of logits at most.
+// Per call without the host, one / split: 128 groups of 4-bit rows (D = 128), 512, 1024,
+// 2048, 4096 keys: 6.4/9.7, 9.0/12.4, 15.9/15.5, 27.0/22.1 us, of bf16 rows 9.6/11.4,
+// 16.4/19.6, 25.7/28.3, 51.8/48.4 us; 8 groups, 4-bit rows, 512, 1024, 2048 keys: 6.3/7.8,
+// 8.7/8.1, 13.5/8.5 us, bf16 8.7/8.3, 14.0/8.6, 22.7/9.1 us.
+bool attend_in_one(int64_t rows, int64_t keys, bool weights, int64_t groups, CacheType type, int head_dim) {
+  const int64_t bytes = type == kCacheFp4 ? 2 * (head_dim + head_dim / 16)
+                                          : head_dim * (type == kCacheF32 ? 8 : 4);
+  return rows <= 16 && keys <= 2048 && (groups >= 128 || keys * bytes <= 288 << 10) &&
+         (!weights || rows * ((keys + 31) / 32 * 32) <= 8192);
 }
 
 // Workgroups a row block's keys are split over: two per CU in all (as many as the
 // registers let run at once), each with 128 keys (one step of every wave) at least.
+// (256, 512, 1024 workgroups in all: 128 groups of 4096 4-bit rows 24.5, 22.2, 26.0 us, of
+// 8192 bf16 rows 113.5, 116.5, 118.3 us; 8 groups of 32768 4-bit rows 16.9, 16.6, 20.8 us.)
 int attend_splits(int64_t blocks, int64_t keys) {
   const int64_t most = std::max<int64_t>(1, (keys + 127) / 128);
   return (int)std::min<int64_t>({std::max<int64_t>(1, 512 / std::max<int64_t>(1, blocks)), most,
@@ -230,7 +240,8 @@ int plan_attend(const ckv_cache *c, const ckv_attend_problem *p, AttendPlan &pl)
   a.logit_stride = round_up(c->capacity, 32);
   a.accumulate = p->accumulate;
   a.masks = p->n_q > 1;
-  a.one = ckv::attend_in_one(rows, c->capacity, true);   // the same bits with and without
+  a.one = ckv::attend_in_one(rows, c->capacity, true,      // the same bits with and without
+                             a.c.groups, (ckv::CacheType)c->dtype, c->head_dim);
   a.splits = a.one ? 1 : ckv::attend_splits((int64_t)a.c.groups * a.row_blocks, c->capacity);
   const float scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)c->head_dim);
   a.c1 = scale * 1.44269504088896340736f;

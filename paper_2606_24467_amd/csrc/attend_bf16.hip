@@ -10,9 +10,11 @@ void launch_attend_bf16(const AttendArgs &a, AttendSource source, int head_dim, 
   };
   auto tiles = [&]<AttendSource SRC, int D, bool MASKS>() {
     if (a.one) go.template operator()<SRC, D, 1, MASKS, true>();
-    else if (a.rt == 1) go.template operator()<SRC, D, 1, MASKS, false>();
-    else if (a.rt == 2) go.template operator()<SRC, D, 2, MASKS, false>();
-    else go.template operator()<SRC, D, 4, MASKS, false>();
+    else if (SRC == kOverWindow || a.rt == 1) go.template operator()<SRC, D, 1, MASKS, false>();
+    else if constexpr (SRC == kOverCache) {      // (more rows over a window: window_prompt.hip)
+      a.rt == 2 ? go.template operator()<SRC, D, 2, MASKS, false>()
+                : go.template operator()<SRC, D, 4, MASKS, false>();
+    }
   };
   auto dim = [&]<AttendSource SRC, bool MASKS>() {
     head_dim == 64 ? tiles.template operator()<SRC, 64, MASKS>()

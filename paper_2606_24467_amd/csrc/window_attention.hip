@@ -26,11 +26,16 @@ struct WindowPlan {
   size_t total() const { return ml_bytes + o_bytes; }
 };
 
-// bf16 calls with more rows per group than this take the kernel for many rows.
-constexpr int64_t kFewRows = 64;
+// bf16 calls with more rows per group than this (a row tile) take the kernel for many
+// rows.  One sequence of 8192 keys, 32 / 8 heads, with 16, 20, 32, 64 rows per group: 16.3, 19.0,
+// 20.5, 40.5 us by the kernel for few, 16.3, 16.6, 17.1, 18.9 us by the one for many; eight:
+// 49.0, 51.5, 52.7, 80.3 and 49.9, 51.5, 52.0, 56.2 us.
+constexpr int64_t kFewRows = 16;
 
 // Workgroups that a row block's keys are split over in the kernel for many
 // rows: as many as two per CU in all leave room for, four tiles each at least.
+// (64 queries over 8192 keys, 32 / 8 heads: 32.6 us; with twice as many workgroups, of two
+// tiles at least, 46.2 us.)
 int prompt_splits(int64_t blocks, int64_t keys) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({512 / blocks, (keys + 255) / 256, 64}));
 }
@@ -96,12 +101,16 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
     return fail(CKV_UNSUPPORTED, "a sequence has 2^31 or more query rows per group");
   pl.prompt = p->dtype == CKV_BF16 && pl.max_rows > kFewRows &&
               std::max(p->k_stride_tok, p->v_stride_tok) * size <= ckv::kPromptMaxStride;
-  a.rt = pl.prompt ? ckv::kPromptRows / 16 : ckv::attend_row_tiles((int)pl.max_rows, false);
+  a.rt = pl.prompt                ? ckv::kPromptRows / 16
+         : p->dtype == CKV_BF16 ? 1
+                                : ckv::attend_row_tiles((int)pl.max_rows, false);
   a.row_blocks = (int32_t)((pl.max_rows + 16 * a.rt - 1) / (16 * a.rt));
   const int64_t blocks = (int64_t)a.c.groups * a.row_blocks;
   if (blocks > 1 << 23) return fail(CKV_UNSUPPORTED, "too many query rows for one launch");
   a.masks = pl.max_rows > a.G;   // more than one token in some row block
-  a.one = !pl.prompt && ckv::attend_in_one(pl.max_rows, keys, false);
+  a.one = !pl.prompt && ckv::attend_in_one(pl.max_rows, keys, false, a.c.groups,
+                                           p->dtype == CKV_F32 ? ckv::kCacheF32 : ckv::kCacheBf16,
+                                           p->head_dim);
   a.splits = pl.prompt ? prompt_splits(pl.blocks, keys)
              : a.one   ? 1
                        : ckv::attend_splits(blocks, keys);

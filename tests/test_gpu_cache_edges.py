@@ -250,3 +250,28 @@ def test_infinities_that_a_row_sees(gpu, dtype, cap):
     assert (out[:, 3] == np.inf).all() and np.isnan(out[:, 9]).all()
     others = np.delete(out, (3, 9), axis=1)
     assert np.isfinite(others).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_windows_over_rows_far_apart(gpu, dtype):
+    """More than 2^24 bytes from one key to the next."""
+    spans = [(20, 70), (1, 9)]
+    q, k, v, cu_q, cu_k = _inputs(spans, 4, 1, 128, dtype, gpu, 70)
+    far = torch.zeros((k.shape[0], (1 << 23) + 64), dtype=dtype, device=gpu)
+    far[:, 64:192], far[:, -128:] = k[:, 0], v[:, 0]
+    kf, vf = far[:, 64:192].unsqueeze(1), far[:, -128:].unsqueeze(1)
+    for sinks in (0, 5):
+        p = C.WindowProblem(q, kf, vf, cu_q, cu_k, window=30, n_sinks=sinks)
+        _check(q, kf, vf, spans, 30, sinks, C.window_attention(p, q, kf, vf))
+
+
+@pytest.mark.parametrize("budget", [2030, 2098])
+def test_evict_of_many_groups(gpu, budget):
+    """More groups than CUs, of more slots than few groups have for the small workgroups."""
+    lengths = [[2100 - (i % 7)] for i in range(300)]
+    cache = H.make_cache(C, BF16, lengths, 2100, 64, gpu, 71)
+    before = H.state(cache)
+    cache.evict(budget, n_sinks=4, n_recent=32)
+    want, got = _evict_oracle(before, budget, 4, 32), H.state(cache)
+    for name in want:
+        assert (got[name] == want[name]).all(), name
