@@ -56,7 +56,7 @@ void launch_attend_join(AttendArgs a, AttendSource source, bool f32, int head_di
 
 // Row tiles per workgroup for that many rows, and workgroups to split `keys` keys
 // of each of `blocks` row blocks over.
-int attend_row_tiles(int rows, bool three_parts);
+int attend_row_tiles(int rows, CacheType type);
 bool attend_in_one(int64_t rows, int64_t keys, bool weights, int64_t groups, CacheType type, int head_dim);
 int attend_splits(int64_t blocks, int64_t keys);
 

@@ -160,10 +160,13 @@ void launch_attend(const AttendArgs &a, AttendSource source, CacheType type, boo
   launch_attend_join(a, source, f32, head_dim, max_rows, stream);
 }
 
-// Row tiles per workgroup: one up to 16 rows, two up to 32, else four (two at
-// most for fp32 queries over 4-bit rows, whose three parts fill the registers).
-int attend_row_tiles(int rows, bool three_parts) {
-  return rows <= 16 ? 1 : rows <= 32 || three_parts ? 2 : 4;
+// Row tiles per workgroup, by what widening or reading the rows again costs against the
+// registers of more tiles (128 groups of 4096 keys, D = 128, 64 rows: one, two, four tiles).
+// 4-bit rows: one (62, 66, 68 us; fp32 queries 72, 86).  fp32 rows: two at most (309, 180,
+// 237 us).  bf16 rows: as many as there are rows for, up to four (155, 89, 77 us).
+int attend_row_tiles(int rows, CacheType type) {
+  const int tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  return type == kCacheFp4 ? 1 : type == kCacheF32 ? std::min(tiles, 2) : tiles;
 }
 
 // Whether one workgroup takes all keys of a group's rows, in one launch, instead of
@@ -235,7 +238,7 @@ int plan_attend(const ckv_cache *c, const ckv_attend_problem *p, AttendPlan &pl)
   a.G = p->n_q_heads / c->n_kv_heads;
   a.n_q = p->n_q;
   a.rows = (int32_t)rows;
-  a.rt = ckv::attend_row_tiles(a.rows, c->dtype == CKV_FP4 && p->dtype == CKV_F32);
+  a.rt = ckv::attend_row_tiles(a.rows, (ckv::CacheType)c->dtype);
   a.row_blocks = (a.rows + 16 * a.rt - 1) / (16 * a.rt);
   a.logit_stride = round_up(c->capacity, 32);
   a.accumulate = p->accumulate;

@@ -11,8 +11,7 @@ void launch_attend_f32(const AttendArgs &a, AttendSource source, int head_dim, d
   auto tiles = [&]<AttendSource SRC, int D, bool MASKS>() {
     if (a.one) go.template operator()<SRC, D, 1, MASKS, true>();
     else if (a.rt == 1) go.template operator()<SRC, D, 1, MASKS, false>();
-    else if (a.rt == 2) go.template operator()<SRC, D, 2, MASKS, false>();
-    else go.template operator()<SRC, D, 4, MASKS, false>();
+    else go.template operator()<SRC, D, 2, MASKS, false>();
   };
   auto dim = [&]<AttendSource SRC, bool MASKS>() {
     head_dim == 64 ? tiles.template operator()<SRC, 64, MASKS>()

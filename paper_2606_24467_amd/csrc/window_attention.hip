@@ -103,7 +103,7 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
               std::max(p->k_stride_tok, p->v_stride_tok) * size <= ckv::kPromptMaxStride;
   a.rt = pl.prompt                ? ckv::kPromptRows / 16
          : p->dtype == CKV_BF16 ? 1
-                                : ckv::attend_row_tiles((int)pl.max_rows, false);
+                                : ckv::attend_row_tiles((int)std::min<int64_t>(pl.max_rows, 64), ckv::kCacheF32);
   a.row_blocks = (int32_t)((pl.max_rows + 16 * a.rt - 1) / (16 * a.rt));
   const int64_t blocks = (int64_t)a.c.groups * a.row_blocks;
   if (blocks > 1 << 23) return fail(CKV_UNSUPPORTED, "too many query rows for one launch");
