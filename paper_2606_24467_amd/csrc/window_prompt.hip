@@ -4,7 +4,7 @@
 // A workgroup takes 32 query rows per wave (row = query token, head of the
 // group, so that the heads of a group share every key) and walks the keys that
 // any of them sees, 64 at a time, through two LDS buffers: while one is worked
-// on, the next tile's loads are in flight to registers.  Products are transposed
+// on, the next tile's loads are in flight to the other.  Products are transposed
 // (S^T = K Q^T, O^T = V^T P^T) on the 32x32x16 instruction: lane 32 h + c holds
 // query row c against the keys 8 (i / 4) + 4 h + i % 4 (element i), which is the
 // order of the reduction slots that P^T goes into the second product with, if V
@@ -13,6 +13,15 @@
 // registers, and the sums of a row belong to the lanes of its column.
 // P is rounded to bf16 once (2^-8 of each probability, as the output itself);
 // its sum is taken before that, in fp32.
+//
+// 32 / 8 heads, D = 128: a prompt of 32768 tokens under a window of 4096 keys 2.12-2.20 ms,
+// 940-975 TFLOP/s of the products that its visible pairs need, where a library product of
+// 8192^3 reaches 1240; 8 prompts of 4096 to 16384 tokens under 1024 keys 1.63-1.67 ms,
+// 805-825 TFLOP/s (the tiles at both ends of a window of 1024 are a tenth more).  The matrix
+// pipe is busy for 45% of the cycles and the vector one for 43%: two waves per SIMD
+// overlap the softmax of one with the products of the other by chance alone.  (One wave that
+// works on the softmax of a tile between the products of its neighbours took 2480 us:
+// its registers did not hold both.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
