@@ -291,23 +291,28 @@ constexpr int kEvictList = 512;     // keys that it ranks against each other, at
 // bits at a time from the top, by counting the keys below three candidates (each
 // wave's by ballots, then one LDS counter each).  No histogram: the weights have
 // few exponents, and all of them would meet in a few bins.  count(t1, t2, t3, n): the
-// wave's keys below each.  counters [16][4] are zero.
-// STEPS < 16: the top 2 STEPS bits alone.
-template <int STEPS, typename F>
-__device__ __forceinline__ uint32_t search_key(F &&count, int (*counters)[4], int drop, int lane, int &less) {
+// wave's keys below each.  counters [16][4] are zero.  STEPS < 16: the top 2 STEPS bits
+// alone.  FEW > 0: ends before, with `bits` bits to go, where at most FEW keys are left in t's
+// range.
+template <int STEPS, int FEW, typename F>
+__device__ __forceinline__ uint32_t search_key(F &&count, int (*counters)[4], int drop, int lane, int &less,
+                                               int &bits) {
   uint32_t t = 0;
   less = 0;
+  int upto = INT32_MAX;          // keys below the range's end
 #pragma unroll 1
-  for (int step = 0; step < STEPS; ++step) {
+  for (int step = 0; step < STEPS && (FEW == 0 || upto - less > FEW); ++step) {
     const int bit = 30 - 2 * step;
     int n[3] = {0, 0, 0};
     count(t | 1u << bit, t | 2u << bit, t | 3u << bit, n);
     if (lane < 3) atomicAdd(&counters[step][lane], lane == 0 ? n[0] : lane == 1 ? n[1] : n[2]);
     __syncthreads();
     const int c1 = counters[step][0], c2 = counters[step][1], c3 = counters[step][2];
+    bits = bit;
     if (c3 < drop) t |= 3u << bit, less = c3;
-    else if (c2 < drop) t |= 2u << bit, less = c2;
-    else if (c1 < drop) t |= 1u << bit, less = c1;
+    else if (c2 < drop) t |= 2u << bit, less = c2, upto = c3;
+    else if (c1 < drop) t |= 1u << bit, less = c1, upto = c2;
+    else upto = c1;
   }
   return t;
 }
@@ -319,13 +324,14 @@ __device__ __forceinline__ uint32_t search_key(F &&count, int (*counters)[4], in
 // 14 bits are searched for: a float to 3%), and the few (key, slot) below the bound
 // are ranked against each other in LDS; so are the freed slots, for their order.
 // Else, or where too many keys are alike: search_key over all keys (in LDS, up to
-// LKEYS of them; else read anew each time), then the freed slots below the budget
+// LKEYS of them; else read anew each time), until those left are few enough to be
+// ranked, then the freed slots below the budget
 // and the kept ones from it on, both ascending, by ballots and prefix sums.
 // FUSED: the moves too; else their lists go to the workspace.
 // Bound by the latency of its phases, one workgroup a group: 512 groups of 4001 slots, one
 // to drop, 6.6 us (16 MB, 2.5 TB/s); 32 groups of 32832 slots, 64 to drop, 17.2 us; 32 of
-// 32768 with 600 to drop, or 64 among many equal ones, 72 and 75 us; 8 of 131072, all but
-// 4072 to drop, 464 us.
+// 32768 with 600 to drop, or 64 among many equal ones, 57 and 75 us (72 and 73 us without
+// ranking the last ones); 8 of 131072, all but 4072 to drop, 364 us (462 us).
 // Loops stay loops: unrolled over a thread's keys in registers, the code that each
 // workgroup runs once took longer to fetch than to run.
 template <int NT, int LKEYS, bool FUSED>
@@ -341,7 +347,8 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
   __shared__ int freed_s[kEvictList];       // of each, its slot if it is freed below the budget
   __shared__ uint8_t tail_gone_s[kFusedMoves];
   __shared__ __align__(16) uint32_t keys_s[LKEYS ? LKEYS : 1];   // of the slots
-  __shared__ int listed_s, moves_s;
+  __shared__ int listed_s, moves_s, less_s;
+  __shared__ uint32_t last_s;
   const int tid = threadIdx.x, lane = tid & 63, bg = blockIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = live_slots(a.c, bg);
@@ -457,7 +464,7 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
   if (tid == 0) listed_s = 0;
   __syncthreads();
   uint32_t t = 0;                // the key of the last slot that goes
-  int less = 0;                  // keys below it
+  int less = 0, bits = 0;        // keys below it; lower bits of it not searched for
   if (drop <= kFusedMoves && drop <= NT / 2) {
     auto count_least = [&](uint32_t t1, uint32_t t2, uint32_t t3, int (&c)[3]) {
       c[0] = __popcll(__ballot(least < t1));
@@ -466,7 +473,7 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
     };
     uint32_t bound = 0xFFFFFFFFu;                // (all keys but the held slots')
     if (n > kEvictList) {
-      bound = search_key<7>(count_least, count_s[0], drop, lane, less) + (1u << 18);
+      bound = search_key<7, 0>(count_least, count_s[0], drop, lane, less, bits) + (1u << 18);
       if (bound == 0u) bound = 0xFFFFFFFFu;
     }
     each_key([&](int slot, uint32_t k) {
@@ -526,7 +533,32 @@ __global__ __launch_bounds__(NT) void evict_kernel(const EvictArgs a) {
       c[2] += __popcll(__ballot(k < t3));
     });
   };
-  t = search_key<16>(count_all, count_s[1], drop, lane, less);
+  t = search_key<16, kEvictList>(count_all, count_s[1], drop, lane, less, bits);
+  if (bits > 0) {                // uniform: the few keys left are ranked
+    if (tid == 0) listed_s = less_s = 0;
+    __syncthreads();
+    each_key([&](int slot, uint32_t k) {
+      if (slot < n && k >= t && (k - t) >> bits == 0) {
+        const int i = atomicAdd(&listed_s, 1);
+        if (i < kEvictList) list_s[i] = (uint64_t)k << 32 | (uint32_t)~slot;
+      }
+    });
+    __syncthreads();
+    const int alike = min(listed_s, kEvictList);
+    for (int i = tid; i < alike; i += NT) {
+      const uint64_t mine = list_s[i];
+      int rank = 0;
+#pragma unroll 8
+      for (int o = 0; o < alike; ++o) rank += list_s[o] < mine;
+      if (rank == drop - less - 1) last_s = (uint32_t)(mine >> 32);
+    }
+    __syncthreads();
+    t = last_s;
+    for (int i = tid; i < alike; i += NT)
+      if ((uint32_t)(list_s[i] >> 32) < t) atomicAdd(&less_s, 1);
+    __syncthreads();
+    less += less_s;
+  }
   // keys below t go, and the highest slots of those equal to it
   int equal = 0;
   each_key([&](int slot, uint32_t k) { equal += __popcll(__ballot(k == t && slot < n)); });
