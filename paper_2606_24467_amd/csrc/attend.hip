@@ -190,10 +190,19 @@ bool attend_in_one(int64_t rows, int64_t keys, bool weights, int64_t groups, Cac
 // registers let run at once), each with 128 keys (one step of every wave) at least.
 // (256, 512, 1024 workgroups in all: 128 groups of 4096 4-bit rows 24.5, 22.2, 26.0 us, of
 // 8192 bf16 rows 113.5, 116.5, 118.3 us; 8 groups of 32768 4-bit rows 16.9, 16.6, 20.8 us.)
+// Where that leaves the last round of workgroups thin (more than half of them row blocks,
+// but no multiple), more splits, of 1024 keys at least, if that takes a quarter off the rounds:
+// 264 groups of up to 6144, 16384 4-bit slots 53.9 -> 44.1, 161 -> 117 us, bf16 161 -> 138,
+// 465 -> 360 us; 320 groups of up to 4096 4-bit slots 40.3 -> 34.6 us.  (Not for less: 400 and
+// 800 groups of up to 4096 41.3 -> 43.0, 84.6 -> 90.2 us.)
 int attend_splits(int64_t blocks, int64_t keys) {
-  const int64_t most = std::max<int64_t>(1, (keys + 127) / 128);
-  return (int)std::min<int64_t>({std::max<int64_t>(1, 512 / std::max<int64_t>(1, blocks)), most,
-                                 (int64_t)kAttendMaxSplits});
+  blocks = std::max<int64_t>(1, blocks);
+  const int64_t first = std::max<int64_t>(1, 512 / blocks), most = std::max<int64_t>(1, (keys + 127) / 128);
+  int64_t best = std::min<int64_t>({first, most, (int64_t)kAttendMaxSplits});
+  auto rounds = [&](int64_t s) { return (blocks * s + 511) / 512; };
+  for (int64_t s = best + 1; s <= std::min<int64_t>(first + 6, kAttendMaxSplits) && s * 1024 <= keys; ++s)
+    if (rounds(s) * best * 4 <= rounds(best) * s * 3) best = s;
+  return (int)best;
 }
 
 }  // namespace ckv
