@@ -648,6 +648,17 @@ _I64x3 = ctypes.c_int64 * 3
 _NO_CONTEXT = contextlib.nullcontext()
 
 
+def _stream_object(device: torch.device, stream) -> torch.cuda.Stream:
+    """The stream that the caller names: a Stream, or a raw handle on the tensors' device.  The
+    handle 0 is the default stream (ExternalStream takes 0 for "none given" and answers
+    with some other stream)."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = int(stream)
+    return (torch.cuda.ExternalStream(handle, device=device) if handle
+            else torch.cuda.default_stream(device))
+
+
 def _enter(device: torch.device, stream):
     """(context, stream handle) of a call on the tensors' device: temporaries and outputs
     are allocated on the stream that the call runs on.  (A decoding step makes
@@ -657,8 +668,7 @@ def _enter(device: torch.device, stream):
         here = torch.cuda.current_device() == index
         return (_NO_CONTEXT if here else torch.cuda.device(device),
                 torch._C._cuda_getCurrentRawStream(index))
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    stream = _stream_object(device, stream)
     if stream.device != device:
         raise ValueError(f"the stream is on {stream.device}, the tensors are on {device}")
     return torch.cuda.stream(stream), stream.cuda_stream
@@ -669,8 +679,7 @@ def _used_on(stream, device: torch.device, *tensors) -> None:
     not given out again before that stream is done with them."""
     if stream is None:
         return
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    stream = _stream_object(device, stream)
     for t in tensors:
         if t is not None and t.numel():
             t.record_stream(stream)

@@ -260,3 +260,15 @@ def test_window_without_queries_needs_no_pointers(L):
     p, keep = _window(cu_k=(0, 0, 0))                     # without keys: q and out still
     assert L.compresskv_window_attention(ctypes.byref(p), FAKE, None, None, None, FAKE, 1 << 40, None) == INV
     assert L.compresskv_window_attention(ctypes.byref(p), None, None, None, FAKE, FAKE, 1 << 40, None) == INV
+
+
+def test_the_handle_0_is_the_default_stream(monkeypatch):
+    """A raw handle may be 0 (the default stream's).  ExternalStream(0) is some other stream:
+    work there is in no order with what the caller has enqueued."""
+    device = torch.device("cuda", 0)
+    asked = []
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda h, device: asked.append(h) or f"handle {h}")
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda d: f"default of {d}")
+    assert C._stream_object(device, 0) == C._stream_object(device, np.int64(0)) == "default of cuda:0"
+    assert not asked
+    assert C._stream_object(device, 0x1234) == "handle 4660"

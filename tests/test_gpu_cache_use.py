@@ -192,3 +192,25 @@ def test_refused_calls_leave_everything(gpu):
     after = H.state(cache)
     for name in before:
         assert (before[name] == after[name]).all(), name
+
+
+def test_calls_on_the_default_stream_by_its_handle(gpu):
+    """stream=0 is the default stream: a call there sees what was enqueued before it, and what
+    is enqueued after sees the call."""
+    assert C._enter(gpu, 0)[1] == torch.cuda.default_stream(gpu).cuda_stream == 0
+    assert C._stream_object(gpu, torch.cuda.default_stream(gpu).cuda_stream) == torch.cuda.default_stream(gpu)
+    side = torch.cuda.Stream(gpu)
+    assert C._enter(gpu, side.cuda_stream)[1] == side.cuda_stream
+    cache = H.make_cache(C, torch.bfloat16, [[60, 40]], 64, 128, gpu, 70)
+    q = torch.randn((1, 1, 8, 128), device=gpu).to(torch.bfloat16)
+    want = cache.attend(q, accumulate=True)
+    weight = cache.weight.clone()
+    cache.weight.zero_()
+    got = cache.attend(q, accumulate=True, stream=0)
+    received = cache.weight.clone()
+    cache.evict(32, n_recent=4, stream=0)
+    torch.cuda.synchronize()
+    assert (H.bits(got) == H.bits(want)).all()
+    live = torch.arange(64, device=gpu) < torch.tensor([[60], [40]], device=gpu)
+    assert (received[0][live] <= weight[0][live]).all() and (received[0][live] > 0).all()
+    assert (cache.length == 32).all()
