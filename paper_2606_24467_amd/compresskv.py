@@ -699,6 +699,14 @@ def _check_tensor(t, name: str, shape, dtype, device) -> None:
         raise ValueError(f"{name} must be on {device}")
 
 
+def _int32(x, name: str) -> int:
+    """x for a 32-bit field of the ABI (ctypes keeps the low bits of a longer one)."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} must fit 32 bits (got {x})")
+    return x
+
+
 def _check_on_gpu(device: torch.device) -> None:
     if device.type != "cuda":
         raise ValueError(f"the tensors must be on a GPU (got {device})")
@@ -876,9 +884,11 @@ class Cache:
               stream=None) -> None:
         """Drops the slots of least weight of every group with more than `budget`."""
         _check_ws(ws, self.device)
+        budget, n_sinks = _int32(budget, "budget"), _int32(n_sinks, "n_sinks")
+        n_recent = _int32(n_recent, "n_recent")
         n = self._evict_bytes.get(budget)
         if n is None:
-            n = lib().compresskv_cache_evict_workspace_bytes(self._ref, int(budget))
+            n = lib().compresskv_cache_evict_workspace_bytes(self._ref, budget)
             if n == 0:
                 raise CompressKVError("compresskv_cache_evict", INVALID_ARGUMENT)
             self._evict_bytes[budget] = n
@@ -887,7 +897,7 @@ class Cache:
             if ws is None:
                 ws = torch.empty(n, dtype=torch.uint8, device=self.device)
             _check("compresskv_cache_evict", lib().compresskv_cache_evict(
-                self._ref, int(budget), int(n_sinks), int(n_recent), ws.data_ptr(),
+                self._ref, budget, n_sinks, n_recent, ws.data_ptr(),
                 ws.numel() * ws.element_size(), handle))
         _used_on(stream, self.device, ws, *self._tensors())
 
@@ -930,7 +940,8 @@ class WindowProblem:
                    for i, w in enumerate(("tok", "head"))}
         self.c = CkvWindowProblem(
             batch=cu_q.shape[0] - 1, n_q_heads=q.shape[1], n_kv_heads=k.shape[1],
-            head_dim=q.shape[2], dtype=_DTYPES[q.dtype], window=int(window), n_sinks=int(n_sinks),
+            head_dim=q.shape[2], dtype=_DTYPES[q.dtype], window=_int32(window, "window"),
+            n_sinks=_int32(n_sinks, "n_sinks"),
             scale=float(scale) if scale else 0.0, cu_q=_ptr(cu_q),
             cu_q_host=self._host[0].ctypes.data, cu_k=_ptr(cu_k),
             cu_k_host=self._host[1].ctypes.data, **strides)

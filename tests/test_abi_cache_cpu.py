@@ -272,3 +272,19 @@ def test_the_handle_0_is_the_default_stream(monkeypatch):
     assert C._stream_object(device, 0) == C._stream_object(device, np.int64(0)) == "default of cuda:0"
     assert not asked
     assert C._stream_object(device, 0x1234) == "handle 4660"
+
+
+def test_integers_past_32_bits_are_refused():
+    """ctypes would keep their low bits: a window of 2^32 + 5 keys would be one of 5."""
+    q, kv = torch.zeros(9, 8, 64), torch.zeros(9, 2, 64)
+    cu = torch.tensor([0, 9], dtype=torch.int32)
+    for bad in (dict(window=(1 << 32) + 5), dict(window=1 << 31), dict(window=4, n_sinks=1 << 32),
+                dict(window=-(1 << 32) + 3)):
+        with pytest.raises(ValueError, match="32 bits"):
+            C.WindowProblem(q, kv, kv, cu, cu, **bad)
+    assert C.WindowProblem(q, kv, kv, cu, cu, window=(1 << 31) - 1).c.window == (1 << 31) - 1
+    cache = C.Cache.__new__(C.Cache)                      # (a cache itself needs a GPU)
+    cache.device = torch.device("cuda", 0)
+    for budget, kw in (((1 << 32) + 8, {}), (8, dict(n_sinks=(1 << 32) + 1)), (8, dict(n_recent=1 << 33))):
+        with pytest.raises(ValueError, match="32 bits"):
+            cache.evict(budget, **kw)
