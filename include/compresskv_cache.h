@@ -99,7 +99,7 @@ typedef struct ckv_attend_problem {
   int32_t n_q;          /* query tokens per sequence, >= 1; n_q * Hq / Hkv <= 64 */
   int32_t dtype;        /* of q and out: CKV_F32 or CKV_BF16; the cache's own unless it is CKV_FP4 */
   int32_t accumulate;   /* 1: add what each slot receives to its weight; 0: leave the weights */
-  float scale;          /* softmax scale; <= 0 selects 1/sqrt(head_dim) */
+  float scale;          /* softmax scale, below 2.3e38; <= 0 selects 1/sqrt(head_dim) */
   int32_t reserved;     /* must be 0 */
 } ckv_attend_problem;
 
@@ -148,7 +148,7 @@ typedef struct ckv_window_problem {
   int32_t dtype;        /* CKV_F32 or CKV_BF16, of q, k, v and out */
   int32_t window;       /* keys that a token sees, itself included, >= 1 */
   int32_t n_sinks;      /* first positions that every later token sees, >= 0 */
-  float scale;          /* softmax scale; <= 0 selects 1/sqrt(head_dim) */
+  float scale;          /* softmax scale, below 2.3e38; <= 0 selects 1/sqrt(head_dim) */
   const int32_t *cu_q, *cu_q_host; /* device and host [batch+1]: query tokens, cu[0] = 0 */
   const int32_t *cu_k, *cu_k_host; /* the same for the keys; non-decreasing both,
                                       at most 2^30 tokens.  The launch is laid out

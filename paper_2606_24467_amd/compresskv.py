@@ -707,6 +707,15 @@ def _int32(x, name: str) -> int:
     return x
 
 
+def _softmax_scale(scale: float | None) -> float:
+    """The ABI's scale: 0 selects 1 / sqrt(head_dim), so no given scale may become 0."""
+    if not scale:
+        return 0.0
+    if scale > 0 and ctypes.c_float(scale).value == 0:
+        raise ValueError(f"scale is 0 in 32 bits (got {scale})")
+    return float(scale)
+
+
 def _check_on_gpu(device: torch.device) -> None:
     if device.type != "cuda":
         raise ValueError(f"the tensors must be on a GPU (got {device})")
@@ -862,7 +871,7 @@ class Cache:
         if known is None:
             a = CkvAttendProblem(n_q_heads=q.shape[2], n_q=q.shape[1], dtype=_row_dtype(q.dtype),
                                  accumulate=int(bool(accumulate)),
-                                 scale=float(scale) if scale else 0.0, reserved=0)
+                                 scale=_softmax_scale(scale), reserved=0)
             n = lib().compresskv_cache_attend_workspace_bytes(self._ref, ctypes.byref(a))
             if n == 0:   # the call itself says why
                 _check("compresskv_cache_attend", lib().compresskv_cache_attend(
@@ -942,7 +951,7 @@ class WindowProblem:
             batch=cu_q.shape[0] - 1, n_q_heads=q.shape[1], n_kv_heads=k.shape[1],
             head_dim=q.shape[2], dtype=_DTYPES[q.dtype], window=_int32(window, "window"),
             n_sinks=_int32(n_sinks, "n_sinks"),
-            scale=float(scale) if scale else 0.0, cu_q=_ptr(cu_q),
+            scale=_softmax_scale(scale), cu_q=_ptr(cu_q),
             cu_q_host=self._host[0].ctypes.data, cu_k=_ptr(cu_k),
             cu_k_host=self._host[1].ctypes.data, **strides)
         self._ref = ctypes.byref(self.c)

@@ -9,6 +9,7 @@ namespace ckv {
 
 constexpr int kAttendWaves = 4;       // waves of a workgroup, each on key steps of its own
 constexpr int kAttendMaxSplits = 256;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // Rows of a group: row r is query token r / G, head g * G + r % G.
 struct AttendArgs {

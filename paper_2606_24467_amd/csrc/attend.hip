@@ -233,7 +233,9 @@ int plan_attend(const ckv_cache *c, const ckv_attend_problem *p, AttendPlan &pl)
   if (p->n_q_heads < 1 || p->n_q_heads % c->n_kv_heads)
     return fail(CKV_INVALID_ARGUMENT, "n_q_heads must be a multiple of n_kv_heads (got %d, %d)",
                 p->n_q_heads, c->n_kv_heads);
-  if (!std::isfinite(p->scale)) return fail(CKV_INVALID_ARGUMENT, "scale must be finite");
+  const float scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)c->head_dim);
+  if (!std::isfinite(p->scale) || !std::isfinite(scale * ckv::kLog2e))
+    return fail(CKV_INVALID_ARGUMENT, "scale must be finite, times log2(e) too");
   if (p->dtype != CKV_F32 && p->dtype != CKV_BF16)
     return fail(CKV_UNSUPPORTED, "queries must be CKV_F32 or CKV_BF16 (got %d)", p->dtype);
   if (c->dtype != CKV_FP4 && p->dtype != c->dtype)
@@ -257,8 +259,7 @@ int plan_attend(const ckv_cache *c, const ckv_attend_problem *p, AttendPlan &pl)
   a.one = ckv::attend_in_one(rows, c->capacity, true,      // the same bits with and without
                              a.c.groups, (ckv::CacheType)c->dtype, c->head_dim);
   a.splits = a.one ? 1 : ckv::attend_splits((int64_t)a.c.groups * a.row_blocks, c->capacity);
-  const float scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)c->head_dim);
-  a.c1 = scale * 1.44269504088896340736f;
+  a.c1 = scale * ckv::kLog2e;
   const size_t parts = (size_t)a.c.groups * a.row_blocks * a.splits * 16 * a.rt;
   pl.ml_bytes = a.splits > 1 || (p->accumulate && !a.one) ? round_up(parts * sizeof(float2), 256) : 0;
   pl.o_bytes = a.splits > 1 ? round_up(parts * c->head_dim * sizeof(float), 256) : 0;

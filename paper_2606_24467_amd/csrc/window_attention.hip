@@ -57,7 +57,9 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
                 p->n_q_heads, p->n_kv_heads);
   if (p->window < 1) return fail(CKV_INVALID_ARGUMENT, "window must be >= 1 (got %d)", p->window);
   if (p->n_sinks < 0) return fail(CKV_INVALID_ARGUMENT, "n_sinks must be >= 0 (got %d)", p->n_sinks);
-  if (!std::isfinite(p->scale)) return fail(CKV_INVALID_ARGUMENT, "scale must be finite");
+  const float scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->head_dim);
+  if (!std::isfinite(p->scale) || !std::isfinite(scale * ckv::kLog2e))
+    return fail(CKV_INVALID_ARGUMENT, "scale must be finite, times log2(e) too");
   if (!p->cu_q || !p->cu_q_host || !p->cu_k || !p->cu_k_host)
     return fail(CKV_INVALID_ARGUMENT, "cu_q, cu_q_host, cu_k and cu_k_host are required");
   int st;
@@ -121,8 +123,7 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
   a.v_tok = p->v_stride_tok * size, a.v_head = p->v_stride_head * size;
   a.cu_q = p->cu_q;
   a.cu_k = p->cu_k;
-  const float scale = p->scale > 0.f ? p->scale : 1.f / sqrtf((float)p->head_dim);
-  a.c1 = scale * 1.44269504088896340736f;
+  a.c1 = scale * ckv::kLog2e;
   const size_t parts = (size_t)a.c.groups * a.row_blocks * a.splits * 16 * a.rt;
   pl.ml_bytes = a.splits > 1 ? round_up(parts * sizeof(float2), 256) : 0;
   pl.o_bytes = a.splits > 1 ? round_up(parts * p->head_dim * sizeof(float), 256) : 0;

@@ -288,3 +288,21 @@ def test_integers_past_32_bits_are_refused():
     for budget, kw in (((1 << 32) + 8, {}), (8, dict(n_sinks=(1 << 32) + 1)), (8, dict(n_recent=1 << 33))):
         with pytest.raises(ValueError, match="32 bits"):
             cache.evict(budget, **kw)
+
+
+def test_scales_that_32_bits_do_not_hold_are_refused(L):
+    """Times log2(e) a scale of 3e38 is infinite, and every zero logit would be NaN; one of 1e-50
+    would be 0, which selects the default."""
+    for scale, ok in ((3e38, False), (2.3e38, True), (1e-45, True), (-3e38, True), (float("inf"), False)):
+        p, keep = _window(scale=scale)
+        assert (L.compresskv_window_attention_workspace_bytes(ctypes.byref(p)) > 0) == ok, scale
+        n = L.compresskv_cache_attend_workspace_bytes(ctypes.byref(_cache()), ctypes.byref(_attend(scale=scale)))
+        assert (n > 0) == ok, scale
+        if not ok:
+            assert b"scale" in L.compresskv_last_error()
+    q, kv = torch.zeros(9, 8, 64), torch.zeros(9, 2, 64)
+    cu = torch.tensor([0, 9], dtype=torch.int32)
+    with pytest.raises(ValueError, match="scale"):
+        C.WindowProblem(q, kv, kv, cu, cu, window=4, scale=1e-50)
+    assert C.WindowProblem(q, kv, kv, cu, cu, window=4, scale=0.0).c.scale == 0
+    assert C.WindowProblem(q, kv, kv, cu, cu, window=4, scale=1e-45).c.scale > 0
