@@ -102,21 +102,33 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, in
     const int s0 = ((int)blockIdx.x - out_blocks) * kJoinSlots;
     if (s0 >= n) return;                          // uniform
     float got[kJoinSlots / 256] = {}, old[kJoinSlots / 256];
+    int32_t pos[kJoinSlots / 256] = {};           // one token sees every slot
 #pragma unroll
-    for (int i = 0; i < kJoinSlots / 256; ++i)
-      old[i] = a.c.weight[(int64_t)bg * a.c.capacity + min(s0 + tid + 256 * i, n - 1)];
+    for (int i = 0; i < kJoinSlots / 256; ++i) {
+      const int64_t at = (int64_t)bg * a.c.capacity + min(s0 + tid + 256 * i, n - 1);
+      old[i] = a.c.weight[at];
+      if (a.masks) pos[i] = a.c.pos[at];
+    }
     join_rows(a, slot0, 0, a.rows, row_s);
     __syncthreads();
     const float *z = a.logits + (int64_t)bg * a.rows * a.logit_stride;
+    // A row whose sum is a NaN gives it to the slots that it sees and to no other: the logit of
+    // those is -infinity, but 0 times a NaN is one.
+    auto add = [&]<bool MASKS>() {
+      int t = (int)((uint32_t)a.c.seen[bg] - (uint32_t)a.n_q), h = 0;   // the row's position, head
 #pragma unroll 4
-    for (int r = 0; r < a.rows; ++r) {
-      const float2 all = row_s[r];
+      for (int r = 0; r < a.rows; ++r) {
+        const float2 all = row_s[r];
 #pragma unroll
-      for (int i = 0; i < kJoinSlots / 256; ++i) {
-        const int s = min(s0 + tid + 256 * i, n - 1);
-        got[i] += fast_exp2(__builtin_fmaf(z[r * a.logit_stride + s], a.c1, -all.x)) * all.y;
+        for (int i = 0; i < kJoinSlots / 256; ++i) {
+          const int s = min(s0 + tid + 256 * i, n - 1);
+          const float p = fast_exp2(__builtin_fmaf(z[r * a.logit_stride + s], a.c1, -all.x)) * all.y;
+          got[i] += !MASKS || pos[i] <= t ? p : 0.f;
+        }
+        if (MASKS && ++h == a.G) h = 0, ++t;
       }
-    }
+    };
+    a.masks ? add.template operator()<true>() : add.template operator()<false>();
 #pragma unroll
     for (int i = 0; i < kJoinSlots / 256; ++i) {
       const int s = s0 + tid + 256 * i;

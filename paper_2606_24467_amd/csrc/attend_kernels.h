@@ -665,11 +665,17 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
   if constexpr (ONE && SRC == kOverCache) {        // (one row block)
     if (a.accumulate)
       for (int x = tid; x < n; x += NTH) {
+        // (a row whose sum is a NaN gives nothing to a slot that it does not see)
+        const int32_t pos = MASKS ? a.c.pos[(int64_t)bg * a.c.capacity + x] : INT32_MIN;
         float got = 0.f;
+        int t = t_first, h = 0;
 #pragma unroll 4
-        for (int r = 0; r < rows; ++r)
-          got += fast_exp2(__builtin_fmaf(logit_s[r * (int)a.logit_stride + x], a.c1, -row_s[r].x)) *
-                 row_s[r].y;
+        for (int r = 0; r < rows; ++r) {
+          const float p = fast_exp2(__builtin_fmaf(logit_s[r * (int)a.logit_stride + x], a.c1, -row_s[r].x)) *
+                          row_s[r].y;
+          got += pos <= t ? p : 0.f;
+          if (++h == a.G) h = 0, ++t;
+        }
         a.c.weight[(int64_t)bg * a.c.capacity + x] += got;
       }
   }

@@ -275,3 +275,35 @@ def test_evict_of_many_groups(gpu, budget):
     want, got = _evict_oracle(before, budget, 4, 32), H.state(cache)
     for name in want:
         assert (got[name] == want[name]).all(), name
+
+
+@pytest.mark.parametrize("dtype,qt", [(FP4, BF16), (FP4, F32), (BF16, BF16), (F32, F32)],
+                         ids=["fp4-bf16", "fp4-f32", "bf16", "f32"])
+@pytest.mark.parametrize("cap", [96, 5024])
+def test_a_row_that_is_not_a_number_gives_nothing_to_slots_it_does_not_see(gpu, dtype, qt, cap):
+    """Of three query tokens the first holds a NaN: it reaches the weights of the slots that the
+    token sees; those of the later tokens get what the later tokens give them."""
+    lengths = [[cap, cap - 33]]
+    cache = H.make_cache(C, dtype, lengths, cap, 128, gpu, 64, past=1000)
+    q = _rows((1, 3, 8, 128), qt, 65, gpu)
+    q[0, 0, 1, 5] = float("nan")                              # a head of the first group
+    before = H.state(cache)
+    out = cache.attend(q, accumulate=True)
+    k, v, qv = H.rows_of(cache, "k"), H.rows_of(cache, "v"), H.values(q)
+    weight = cache.weight.cpu().numpy().astype(np.float64)
+    for g in range(2):
+        n, seen = lengths[0][g], before["seen"][0, g]
+        pos = before["pos"][0, g, :n]
+        qg = qv[0, :, 4 * g:4 * g + 4]
+        _, want, p, sees = CO.attend(qg, k[0, g, :n], v[0, g, :n], pos, seen)
+        assert np.isnan(want).sum() == (0 if g else n - 2)    # two slots are later tokens'
+        assert (np.isnan(weight[0, g, :n]) == np.isnan(want)).all()
+        fine = ~np.isnan(want)
+        old = before["weight"][0, g].view(np.float32)[:n].astype(np.float64)
+        with np.errstate(invalid="ignore"):
+            dz = H.logit_error(qg, k[0, g, :n], 128 ** -0.5)
+            p, dz = np.where(np.isnan(p), 0.0, p), np.where(np.isnan(dz), 0.0, dz)
+        err = 2 * np.where(sees, dz, 0).max(-1, initial=0)[..., None] + 2 * n * H.U + 2.0 ** -22
+        tol = (p * err).sum((0, 1)) + H.U * (12 * np.nan_to_num(want) + old + np.nan_to_num(want))
+        assert (np.abs(weight[0, g, :n] - old - want) <= tol + 1e-30)[fine].all(), g
+    assert np.isnan(H.values(out)[0, 0, 1]).all() and np.isfinite(H.values(out)[0, 1:]).all()
