@@ -172,7 +172,11 @@ size_t compresskv_window_attention_workspace_bytes(const ckv_window_problem *p);
  * are not written.  Sums and softmax are held in fp32; K and V of a key that a
  * query does not see do not reach it, whatever they hold.  Without any query
  * nothing is done, and q and out may be NULL; without any key k and v may be.
- * ws: >= compresskv_window_attention_workspace_bytes(), 256-byte aligned.
+ * Refused besides: 2^31 query rows (tokens times Hq / Hkv) or more in one sequence, and
+ * more than 2^24 - 512 blocks of query rows in all; a block is 128 rows (bf16, more than 16
+ * rows in some sequence, and tokens of K and V at most 2^24 bytes apart) or else 16 or 32.
+ * ws: >= compresskv_window_attention_workspace_bytes(), 256-byte aligned; none (256
+ * bytes) where no row is split over workgroups.
  */
 int compresskv_window_attention(const ckv_window_problem *p, const void *q, const void *k,
                                 const void *v, void *out, void *ws, size_t ws_bytes, void *stream);

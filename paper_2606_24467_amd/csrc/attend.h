@@ -19,15 +19,18 @@ struct AttendArgs {
   const char *k, *v;                  // window: packed rows
   int64_t q_tok, q_head, k_tok, k_head, v_tok, v_head;   // window: byte strides
   const int32_t *cu_q, *cu_k;         // window
-  float2 *part_ml;                    // [groups][row_blocks][splits][16 RT] (reference, sum)
-  float *part_o;                      // [groups][row_blocks][splits][16 RT][D]
+  float2 *part_ml;                    // [blocks][splits][16 RT] (reference, sum)
+  float *part_o;                      // [blocks][splits][16 RT][D]
   float *logits;                      // accumulate (several splits): [groups][rows][logit_stride]
                                       // raw q . k
   int64_t logit_stride;
   int32_t Hkv, G, n_q;                // n_q: cache only
   int32_t rows;                       // cache: n_q * G
   int32_t rt;                         // row tiles per workgroup: 1, 2 or 4
-  int32_t row_blocks, splits;
+  int32_t row_blocks, splits;         // row_blocks: of the group with the most rows
+  int32_t blocks;                     // row blocks of all groups
+  int32_t packed;                     // window: some group has fewer than row_blocks, and the
+                                      // blocks are numbered without gaps (row_blocks.h)
   int32_t accumulate;                 // cache: add to the weights
   int32_t masks;                      // rows of a workgroup may see different keys
   int32_t join_rows;                  // rows per workgroup of the join (set by its launcher)
@@ -49,7 +52,7 @@ void launch_attend(const AttendArgs &a, AttendSource source, CacheType type, boo
 // that many 16-row tiles.
 constexpr int kPromptRows = 128;
 constexpr int64_t kPromptMaxStride = 1 << 24;   // bytes between tokens: 64 rows stay within 32 bits
-void launch_window_prompt(const AttendArgs &a, int head_dim, int blocks, int max_rows, hipStream_t stream);
+void launch_window_prompt(const AttendArgs &a, int head_dim, int max_rows, hipStream_t stream);
 
 // Joins the splits' outputs, and adds to the weights if a.accumulate.
 void launch_attend_join(AttendArgs a, AttendSource source, bool f32, int head_dim,

@@ -8,6 +8,7 @@
 
 #include "attend.h"
 #include "cache_api.h"
+#include "row_blocks.h"
 #include "score_common.h"
 
 namespace ckv {
@@ -44,7 +45,8 @@ __device__ __forceinline__ void join_rows(const AttendArgs &a, int64_t slot0, in
 
 constexpr int kJoinSlots = 1024;   // slots whose weights one workgroup adds to
 
-// Grid (out_blocks + weight blocks, groups), 256 threads.  The first out_blocks
+// Grid (out_blocks + weight blocks, groups), or where the row blocks are packed (row
+// blocks * workgroups of each, 1), 256 threads.  The first out_blocks
 // join the splits' outputs, up to 1024 / D rows each: D / 4 lanes per row, and where
 // that leaves lanes (few rows, many splits) the splits are dealt to several such
 // parts, whose sums are added in order.  Each of the others adds to the
@@ -55,15 +57,24 @@ constexpr int kJoinSlots = 1024;   // slots whose weights one workgroup adds to
 template <AttendSource SRC, typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, int out_blocks) {
   const int tid = threadIdx.x, bg = blockIdx.y, RM = 16 * a.rt;
-  const int b = bg / a.Hkv, g = bg - b * a.Hkv;
-  const int64_t slot0 = (int64_t)bg * a.row_blocks * a.splits;
+  int b = bg / a.Hkv, g = bg - b * a.Hkv, r0 = (int)blockIdx.x * a.join_rows;
+  int64_t slot0 = (int64_t)bg * a.row_blocks * a.splits;   // of the group's first row block
+  if constexpr (SRC == kOverWindow) {
+    if (a.packed) {
+      const int each = RM / a.join_rows, id = (int)blockIdx.x / each;
+      RowBlock found;
+      if (!find_row_block<false>(a, id, RM, found)) return;   // uniform
+      b = found.b, g = found.g;
+      r0 = found.rb * RM + ((int)blockIdx.x - id * each) * a.join_rows;
+      slot0 = (int64_t)(found.part - found.rb) * a.splits;
+    }
+  }
   if ((int)blockIdx.x < out_blocks) {
     constexpr int LR = D / 4, NP = 256 / LR;      // lanes per row; rows x parts of the splits
     __shared__ __align__(16) f32x4 part_s[NP][LR];
     __shared__ float2 all_s[NP];
     const int q0 = SRC == kOverWindow ? a.cu_q[b] : 0;
     const int rows = SRC == kOverWindow ? (a.cu_q[b + 1] - q0) * a.G : a.rows;
-    const int r0 = (int)blockIdx.x * a.join_rows;
     if (r0 >= rows) return;                       // uniform
     const int here = min(a.join_rows, rows - r0), parts = NP / a.join_rows;
     join_rows(a, slot0, r0, here, all_s);
@@ -142,10 +153,12 @@ void launch_attend_join(AttendArgs a, AttendSource source, bool f32, int head_di
   // rows per workgroup: as many as fill it, fewer where the splits are many
   a.join_rows = 1024 / head_dim;
   while (a.join_rows > 1 && a.splits > 4 * (1024 / head_dim / a.join_rows)) a.join_rows /= 2;
-  const int out_blocks = a.splits > 1 ? (max_rows + a.join_rows - 1) / a.join_rows : 0;
+  const int out_blocks = a.splits == 1 ? 0
+                         : a.packed    ? a.blocks * (16 * a.rt / a.join_rows)
+                                       : (max_rows + a.join_rows - 1) / a.join_rows;
   const int weight_blocks = a.accumulate && !a.one ? (a.c.capacity + kJoinSlots - 1) / kJoinSlots : 0;
   if (out_blocks + weight_blocks == 0) return;
-  const dim3 grid(out_blocks + weight_blocks, a.c.groups);
+  const dim3 grid(out_blocks + weight_blocks, a.packed ? 1 : a.c.groups);
   auto go = [&]<AttendSource SRC, typename T, int D>() {
     hipLaunchKernelGGL((attend_join_kernel<SRC, T, D>), grid, dim3(256), 0, stream, a, out_blocks);
   };
@@ -167,7 +180,7 @@ void launch_attend_f32(const AttendArgs &a, AttendSource source, int head_dim, d
 
 void launch_attend(const AttendArgs &a, AttendSource source, CacheType type, bool f32, int head_dim,
                    int max_rows, hipStream_t stream) {
-  const dim3 grid(a.row_blocks, a.c.groups, a.splits);
+  const dim3 grid = a.packed ? dim3(a.blocks, 1, a.splits) : dim3(a.row_blocks, a.c.groups, a.splits);
   if (type == kCacheFp4) launch_attend_fp4(a, f32, head_dim, grid, stream);
   else if (type == kCacheBf16) launch_attend_bf16(a, source, head_dim, grid, stream);
   else launch_attend_f32(a, source, head_dim, grid, stream);
@@ -265,14 +278,15 @@ int plan_attend(const ckv_cache *c, const ckv_attend_problem *p, AttendPlan &pl)
   a.rows = (int32_t)rows;
   a.rt = ckv::attend_row_tiles(a.rows, (ckv::CacheType)c->dtype);
   a.row_blocks = (a.rows + 16 * a.rt - 1) / (16 * a.rt);
+  a.blocks = a.c.groups * a.row_blocks;
   a.logit_stride = round_up(c->capacity, 32);
   a.accumulate = p->accumulate;
   a.masks = p->n_q > 1;
   a.one = ckv::attend_in_one(rows, c->capacity, true,      // the same bits with and without
                              a.c.groups, (ckv::CacheType)c->dtype, c->head_dim);
-  a.splits = a.one ? 1 : ckv::attend_splits((int64_t)a.c.groups * a.row_blocks, c->capacity);
+  a.splits = a.one ? 1 : ckv::attend_splits(a.blocks, c->capacity);
   a.c1 = scale * ckv::kLog2e;
-  const size_t parts = (size_t)a.c.groups * a.row_blocks * a.splits * 16 * a.rt;
+  const size_t parts = (size_t)a.blocks * a.splits * 16 * a.rt;
   pl.ml_bytes = a.splits > 1 || (p->accumulate && !a.one) ? round_up(parts * sizeof(float2), 256) : 0;
   pl.o_bytes = a.splits > 1 ? round_up(parts * c->head_dim * sizeof(float), 256) : 0;
   pl.logit_bytes =

@@ -35,6 +35,7 @@
 #pragma once
 
 #include "attend.h"
+#include "row_blocks.h"
 #include "score_common.h"
 
 namespace ckv {
@@ -123,8 +124,17 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 15, quad = lane >> 4;
-  const int bg = blockIdx.y, rb = blockIdx.x, split = blockIdx.z;
-  const int b = bg / a.Hkv, g = bg - b * a.Hkv;
+  const int split = blockIdx.z;
+  int rb = blockIdx.x, b = (int)blockIdx.y / a.Hkv, g = (int)blockIdx.y - b * a.Hkv;
+  int part = (int)blockIdx.y * a.row_blocks + rb;   // the row block's number
+  if constexpr (SRC == kOverWindow && MASKS && !ONE) {
+    if (a.packed) {
+      RowBlock found;
+      if (!find_row_block<false>(a, rb, RM, found)) return;   // uniform
+      rb = found.rb, b = found.b, g = found.g, part = found.part;
+    }
+  }
+  const int bg = b * a.Hkv + g;
 
   // the rows of this workgroup and the keys that any of them sees
   int rows, n, t_first = 0, t_last = 0, lo = 0, sinks = 0;
@@ -603,7 +613,7 @@ __global__ __launch_bounds__(64 * (ONE ? 2 : 1) * kAttendWaves) void attend_kern
     if (quad == 0) ml_s[wave][16 * rt + c] = make_float2(m[rt], l[rt]);
   }
   __syncthreads();
-  const int64_t slot = ((int64_t)bg * a.row_blocks + rb) * a.splits + split;
+  const int64_t slot = (int64_t)part * a.splits + split;
   if (tid < RM) {
     float top = -INFINITY;
 #pragma unroll

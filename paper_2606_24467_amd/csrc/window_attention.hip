@@ -16,11 +16,13 @@ using ckv_api::round_up;
 namespace {
 
 constexpr int32_t kMaxTokens = 1 << 30;
+// Row blocks of a call: 256 threads each, and a launch has 2^32 at most (the kernel for
+// many rows rounds up by 255 blocks).
+constexpr int64_t kMaxBlocks = (1 << 24) - 512;
 
 struct WindowPlan {
   ckv::AttendArgs a;
   int64_t max_rows;             // query rows of one (sequence, group)
-  int64_t blocks;               // row blocks of all, where the kernel for many rows takes them
   bool prompt;                  // the kernel for many rows
   size_t ml_bytes, o_bytes;
   size_t total() const { return ml_bytes + o_bytes; }
@@ -88,14 +90,13 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
   a.c.groups = p->batch * p->n_kv_heads;
   a.Hkv = p->n_kv_heads;
   a.G = p->n_q_heads / p->n_kv_heads;
-  pl.max_rows = pl.blocks = 0;
+  pl.max_rows = 0;
   int64_t keys = 0;              // that a row block may read, at most
   for (int b = 0; b < p->batch; ++b) {
     const int64_t lq = p->cu_q_host[b + 1] - p->cu_q_host[b];
     const int64_t lk = p->cu_k_host[b + 1] - p->cu_k_host[b];
     if (lq == 0) continue;
     pl.max_rows = std::max(pl.max_rows, lq * a.G);
-    pl.blocks += (lq * a.G + ckv::kPromptRows - 1) / ckv::kPromptRows * a.Hkv;
     const int64_t span = std::min<int64_t>(lq, ckv::kPromptRows / a.G + 1);   // tokens of a block
     keys = std::max(keys, std::min<int64_t>(lk, (int64_t)p->window + p->n_sinks + span - 1));
   }
@@ -107,13 +108,25 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
          : p->dtype == CKV_BF16 ? 1
                                 : ckv::attend_row_tiles((int)std::min<int64_t>(pl.max_rows, 64), ckv::kCacheF32);
   a.row_blocks = (int32_t)((pl.max_rows + 16 * a.rt - 1) / (16 * a.rt));
-  const int64_t blocks = (int64_t)a.c.groups * a.row_blocks;
-  if (blocks > 1 << 23) return fail(CKV_UNSUPPORTED, "too many query rows for one launch");
   a.masks = pl.max_rows > a.G;   // more than one token in some row block
   a.one = !pl.prompt && ckv::attend_in_one(pl.max_rows, keys, false, a.c.groups,
                                            p->dtype == CKV_F32 ? ckv::kCacheF32 : ckv::kCacheBf16,
                                            p->head_dim);
-  a.splits = pl.prompt ? prompt_splits(pl.blocks, keys)
+  // The row blocks that there are, where one per group is not all: sequences of other lengths
+  // beside a long one cost no workgroups and no workspace then.
+  const int64_t most = (int64_t)a.c.groups * a.row_blocks;
+  int64_t blocks = most;
+  if (pl.prompt || (a.masks && !a.one)) {
+    blocks = 0;
+    for (int b = 0; b < p->batch; ++b) {
+      const int64_t rows = (int64_t)(p->cu_q_host[b + 1] - p->cu_q_host[b]) * a.G;
+      blocks += (rows + 16 * a.rt - 1) / (16 * a.rt) * a.Hkv;
+    }
+  }
+  if (blocks > kMaxBlocks) return fail(CKV_UNSUPPORTED, "too many query rows for one launch");
+  a.blocks = (int32_t)blocks;
+  a.packed = blocks < most;
+  a.splits = pl.prompt ? prompt_splits(blocks, keys)
              : a.one   ? 1
                        : ckv::attend_splits(blocks, keys);
   a.window = std::min(p->window, kMaxTokens);   // positions plus or minus either stay in 32 bits
@@ -124,7 +137,7 @@ int plan_window(const ckv_window_problem *p, WindowPlan &pl) {
   a.cu_q = p->cu_q;
   a.cu_k = p->cu_k;
   a.c1 = scale * ckv::kLog2e;
-  const size_t parts = (size_t)a.c.groups * a.row_blocks * a.splits * 16 * a.rt;
+  const size_t parts = (size_t)a.blocks * a.splits * 16 * a.rt;
   pl.ml_bytes = a.splits > 1 ? round_up(parts * sizeof(float2), 256) : 0;
   pl.o_bytes = a.splits > 1 ? round_up(parts * p->head_dim * sizeof(float), 256) : 0;
   return CKV_OK;
@@ -171,7 +184,7 @@ int compresskv_window_attention(const ckv_window_problem *p, const void *q, cons
   a.part_o = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.ml_bytes);
   const bool f32 = p->dtype == CKV_F32;
   if (pl.prompt)
-    ckv::launch_window_prompt(a, p->head_dim, (int)pl.blocks, (int)pl.max_rows, (hipStream_t)stream);
+    ckv::launch_window_prompt(a, p->head_dim, (int)pl.max_rows, (hipStream_t)stream);
   else
     ckv::launch_attend(a, ckv::kOverWindow, f32 ? ckv::kCacheF32 : ckv::kCacheBf16, f32, p->head_dim,
                        (int)pl.max_rows, (hipStream_t)stream);

@@ -27,6 +27,7 @@
 #include <algorithm>
 
 #include "attend.h"
+#include "row_blocks.h"
 #include "score_common.h"
 
 namespace ckv {
@@ -59,8 +60,7 @@ __device__ __forceinline__ void add_unbounded32(f32x16 &acc, bf16x8 &v, bf16x8 s
 }
 
 template <int D>
-__global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(const AttendArgs a, int blocks,
-                                                                            int run) {
+__global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(const AttendArgs a, int run) {
   constexpr int NF = D / 16, DB = D / 32;        // K fragments, blocks of 32 head dimensions
   constexpr int U = D / 8;                       // 16-byte units per row
   constexpr int LD = kPromptKeys * U / (64 * kPromptWaves);   // loads of K (of V) per wave and tile
@@ -76,70 +76,17 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 31, h = lane >> 5;
 
-  // The row blocks that there are, sequence by sequence and group by group, are
-  // numbered without gaps.  Consecutive ones share their keys, so runs of them go to
+  // Consecutive row blocks share their keys, so runs of them go to
   // one XCD (workgroups go round the XCDs in turn) and the runs go round the XCDs, the
-  // latest rows of a group first.  Each wave finds its sequence: the lanes look at 64
-  // runs of sequences together, then at the sequences of a run.  (8 prompts of 4k to
+  // latest rows of a group first.  Each wave finds its sequence.  (8 prompts of 4k to
   // 16k tokens: 1810 us with a grid over the longest one's blocks for each, most XCDs
-  // waiting for the one with the most rows, 1700 so.  4096 sequences of 64 tokens:
-  // 772 us looked for 64 sequences after the other, 454 so.)
+  // waiting for the one with the most rows, 1700 so.)
   const int in_xcd = (int)blockIdx.x >> 3;
-  int id = (in_xcd / run * 8 + ((int)blockIdx.x & 7)) * run + in_xcd % run;
-  if (id >= blocks) return;                      // uniform
-  const int batch = a.c.groups / a.Hkv;
-  auto blocks_of = [&](int tokens) {             // of a sequence, per group
-    const int64_t n = ((int64_t)tokens * a.G + kPromptRows - 1) / kPromptRows;
-    return (int)max((int64_t)0, min(n, (int64_t)a.row_blocks));
-  };
-  auto scan = [&](int x) {                       // inclusive, over the lanes
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      const int before = __shfl_up(x, o);
-      x += lane >= o ? before : 0;
-    }
-    return x;
-  };
-  int b0 = 0;
-  if (batch > 64) {                              // first a run of sequences a lane
-    const int per = (batch + 63) / 64, from = min(lane * per, batch), to = min(from + per, batch);
-    int mine = 0, at = a.cu_q[from];
-#pragma unroll 8
-    for (int i = from; i < to; ++i) {
-      const int next = a.cu_q[i + 1];
-      mine += blocks_of(next - at);
-      at = next;
-    }
-    const int upto = scan(mine * a.Hkv);
-    const uint64_t beyond = __ballot(upto > id);
-    if (beyond == 0) return;                     // uniform
-    const int src = __builtin_ctzll(beyond);
-    id -= __builtin_amdgcn_readlane(upto - mine * a.Hkv, src);
-    b0 = src * per;
-  }
-  int b = -1, nb = 0, q0 = 0, k0 = 0, lq = 0, lk = 0;
-  for (; b0 < batch; b0 += 64) {
-    const int at = min(b0 + lane, batch - 1);
-    const int q_at = a.cu_q[at], q_to = a.cu_q[at + 1], k_at = a.cu_k[at], k_to = a.cu_k[at + 1];
-    const int mine = b0 + lane < batch ? blocks_of(q_to - q_at) : 0;
-    const int upto = scan(mine * a.Hkv);
-    const uint64_t beyond = __ballot(upto > id);
-    if (beyond == 0) {
-      id -= __builtin_amdgcn_readlane(upto, 63);
-      continue;
-    }
-    const int src = __builtin_ctzll(beyond);
-    b = b0 + src;
-    nb = __builtin_amdgcn_readlane(mine, src);
-    id -= __builtin_amdgcn_readlane(upto, src) - nb * a.Hkv;
-    q0 = __builtin_amdgcn_readlane(q_at, src);
-    k0 = __builtin_amdgcn_readlane(k_at, src);
-    lq = __builtin_amdgcn_readlane(q_to, src) - q0;
-    lk = __builtin_amdgcn_readlane(k_to, src) - k0;
-    break;
-  }
-  if (b < 0) return;                             // uniform
-  const int g = id / nb, rb = nb - 1 - (id - g * nb), bg = b * a.Hkv + g;
+  const int id = (in_xcd / run * 8 + ((int)blockIdx.x & 7)) * run + in_xcd % run;
+  if (id >= a.blocks) return;                     // uniform
+  RowBlock at;
+  if (!find_row_block<true>(a, id, kPromptRows, at)) return;   // uniform
+  const int g = at.g, rb = at.rb, q0 = at.q0, lq = at.lq, k0 = at.k0, lk = at.lk;
   const int rows = lq * a.G, r0 = rb * kPromptRows;
   const int t0 = lk - lq;                        // position of query token 0
   const int t_first = t0 + r0 / a.G, t_last = t0 + (min(rows, r0 + kPromptRows) - 1) / a.G;
@@ -402,7 +349,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
   if (a.splits > 1) {                            // joined by attend_join_kernel
-    const int64_t slot = ((int64_t)bg * a.row_blocks + rb) * a.splits + split;
+    const int64_t slot = (int64_t)at.part * a.splits + split;
     const int64_t row = slot * kPromptRows + 32 * wave + c;
     if (in) {
       if (h == 0) a.part_ml[row] = make_float2(m, l);
@@ -441,15 +388,15 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void window_prompt_kernel(con
   }
 }
 
-void launch_window_prompt(const AttendArgs &a, int head_dim, int blocks, int max_rows, hipStream_t stream) {
+void launch_window_prompt(const AttendArgs &a, int head_dim, int max_rows, hipStream_t stream) {
   // 32 row blocks (half of what an XCD holds at a time) in a run, fewer where that
   // would leave an XCD with less than about 16 runs
-  const int run = std::clamp(blocks / 128, 1, 32);
-  const dim3 grid((unsigned)(((int64_t)blocks + 8 * run - 1) / (8 * run) * (8 * run)), a.splits);
+  const int run = std::clamp(a.blocks / 128, 1, 32);
+  const dim3 grid((unsigned)(((int64_t)a.blocks + 8 * run - 1) / (8 * run) * (8 * run)), a.splits);
   if (head_dim == 64)
-    hipLaunchKernelGGL((window_prompt_kernel<64>), grid, dim3(64 * kPromptWaves), 0, stream, a, blocks, run);
+    hipLaunchKernelGGL((window_prompt_kernel<64>), grid, dim3(64 * kPromptWaves), 0, stream, a, run);
   else
-    hipLaunchKernelGGL((window_prompt_kernel<128>), grid, dim3(64 * kPromptWaves), 0, stream, a, blocks, run);
+    hipLaunchKernelGGL((window_prompt_kernel<128>), grid, dim3(64 * kPromptWaves), 0, stream, a, run);
   launch_attend_join(a, kOverWindow, false, head_dim, max_rows, stream);
 }
 

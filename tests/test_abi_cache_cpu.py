@@ -306,3 +306,33 @@ def test_scales_that_32_bits_do_not_hold_are_refused(L):
         C.WindowProblem(q, kv, kv, cu, cu, window=4, scale=1e-50)
     assert C.WindowProblem(q, kv, kv, cu, cu, window=4, scale=0.0).c.scale == 0
     assert C.WindowProblem(q, kv, kv, cu, cu, window=4, scale=1e-45).c.scale > 0
+
+
+def _window_bytes(L, spans, hq=32, hkv=8, dtype=C.BF16, **kw):
+    """Workspace of dense sequences of (queries, keys); 0: refused."""
+    cu = [tuple(int(x) for x in np.cumsum([0] + [s[i] for s in spans])) for i in (0, 1)]
+    p, keep = _window(cu_q=cu[0], cu_k=cu[1], batch=len(spans), n_q_heads=hq, n_kv_heads=hkv, dtype=dtype,
+                      window=1024, **kw)
+    return L.compresskv_window_attention_workspace_bytes(ctypes.byref(p))
+
+
+def test_windows_of_sequences_of_very_different_lengths_are_taken(L):
+    """The limit counts the row blocks that there are, not the longest sequence's for every group."""
+    assert _window_bytes(L, [(1, 1)] * 300 + [(131072, 131072)]) == 256
+    assert _window_bytes(L, [(1, 1)] * 1000 + [(40000, 40000)]) == 256
+    assert _window_bytes(L, [(1, 1)] * 65 + [(131072, 131072)], dtype=C.F32) == 256
+    assert _window_bytes(L, [(1, 1)] * 4000 + [(1 << 20, 1 << 20)], dtype=C.F32) == 256
+    assert _window_bytes(L, [(1 << 30, 1 << 30)], hq=1, hkv=1) == 256
+    assert _window_bytes(L, [(1 << 30, 1 << 30)], hq=2, hkv=2) == 0
+    assert b"rows" in L.compresskv_last_error()
+
+
+@pytest.mark.parametrize("dtype", [C.BF16, C.F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("apart", [512, 1 << 24], ids=["near", "far"])
+def test_windows_of_sequences_without_queries_cost_no_workspace(L, dtype, apart):
+    """A chunk split over workgroups needs the same workspace alone and among empty sequences."""
+    kw = dict(dtype=dtype, k_stride_tok=apart)
+    alone = _window_bytes(L, [(64, 4096)], **kw)
+    assert alone > 256
+    assert _window_bytes(L, [(0, 0)] * 255 + [(64, 4096)], **kw) == alone
+    assert _window_bytes(L, [(0, 50)] * 8000 + [(64, 4096)] + [(0, 0)] * 100, **kw) == alone

@@ -154,3 +154,52 @@ def test_window_attention_of_thousands_of_sequences(gpu):
     out = C.window_attention(p, q, k, v)
     keep = [s for s in spans if s[0]]
     _check(q, k, v, keep, 20, 2, out)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_windows_of_mixed_lengths(gpu, dtype, d):
+    """Long chunks beside single tokens and sequences without any query, each row block split
+    over workgroups: their numbering and their join leave out what is not there."""
+    spans = [(0, 9)] * 3 + [(1, 300)] * 5 + [(70, 900)] + [(0, 0)] * 70 + [(3, 40), (0, 5), (33, 700)]
+    q, k, v, cu_q, cu_k = _inputs(spans, 8, 2, d, dtype, gpu, 15)
+    for window, sinks in ((400, 3), (1 << 20, 0)):
+        p = C.WindowProblem(q, k, v, cu_q, cu_k, window=window, n_sinks=sinks)
+        assert p._ws_bytes > 256                              # split
+        out = torch.full_like(q, 7.0)
+        C.window_attention(p, q, k, v, out=out)
+        _check(q, k, v, spans, window, sinks, out)
+        assert (out[sum(s[0] for s in spans):] == 7.0).all()
+        again = torch.full_like(q, 7.0)
+        C.window_attention(p, q, k, v, out=again)
+        assert (H.bits(again) == H.bits(out)).all()
+
+
+def test_windows_of_mixed_lengths_over_rows_far_apart(gpu):
+    """The same in the kernel for few rows, which bf16 rows far apart take."""
+    spans = [(0, 2)] * 70 + [(1, 20)] * 3 + [(20, 300), (0, 0), (5, 9)]
+    q, k, v, cu_q, cu_k = _inputs(spans, 4, 1, 128, BF16, gpu, 16)
+    far = torch.zeros((k.shape[0], (1 << 23) + 64), dtype=BF16, device=gpu)
+    far[:, 64:192], far[:, -128:] = k[:, 0], v[:, 0]
+    kf, vf = far[:, 64:192].unsqueeze(1), far[:, -128:].unsqueeze(1)
+    p = C.WindowProblem(q, kf, vf, cu_q, cu_k, window=250, n_sinks=5)
+    assert p._ws_bytes > 256
+    _check(q, kf, vf, spans, 250, 5, C.window_attention(p, q, kf, vf))
+
+
+@pytest.mark.parametrize("dtype,singles", [(BF16, 300), (F32, 65)], ids=["bf16", "f32"])
+def test_a_long_prompt_beside_single_tokens(gpu, dtype, singles):
+    """Far more row blocks in one sequence than in the others."""
+    n, window, hq, hkv, d = 131072, 19, 32, 8, 64
+    spans = [(1, 30)] * singles + [(n, n)]
+    print("long prompt", dtype, singles, file=sys.stderr, flush=True)
+    q, k, v, cu_q, cu_k = _inputs(spans, hq, hkv, d, dtype, gpu, 17)
+    p = C.WindowProblem(q, k, v, cu_q, cu_k, window=window)
+    out = C.window_attention(p, q, k, v)
+    tq, tk = singles + n, 30 * singles + n
+    assert torch.isfinite(out[:tq]).all()
+    _check(q[:singles], k[:30 * singles], v[:30 * singles], spans[:singles], window, 0, out[:singles])
+    for at in (0, 40000, n - 150):                            # pieces of the long one
+        back = min(at, window - 1)
+        qs, ks = slice(singles + at, singles + at + 150), slice(tk - n + at - back, tk - n + at + 150)
+        _check(q[qs], k[ks], v[ks], [(150, 150 + back)], window, 0, out[qs])
