@@ -112,10 +112,11 @@ size_t compresskv_cache_attend_workspace_bytes(const ckv_cache *c, const ckv_att
  * One query token attends to every live slot; of n_q > 1, the last n_q tokens
  * of the sequence, token i attends to the slots at positions <= seen - n_q + i
  * (their own rows have been appended before).  A row that sees no slot gives
- * zeros.  With accumulate, weight_s += sum over i and the heads h of the group
- * of p(i, h, s), added in fp32.
- * q, out: [batch][n_q][Hq][D], 16-byte aligned.  Sums and softmax are held in
- * fp32; see the kernel for what is rounded before a matrix product.  K and V of
+ * zeros, and so does one whose every visible logit is -infinity.  With accumulate,
+ * weight_s += sum over i and the heads h of the group of p(i, h, s), added in fp32.
+ * q, out: [batch][n_q][Hq][D], 16-byte aligned.  Logits, sums and softmax are held
+ * in fp32.  Before the product with V a probability is rounded to 16 bits (bf16
+ * queries; the output's own rounding is 2^8 times as coarse) or to 24.  K and V of
  * slots past len, and of slots that a row does not see, do not reach that row,
  * whatever they hold.
  * ws: >= compresskv_cache_attend_workspace_bytes(), 256-byte aligned.
@@ -130,10 +131,10 @@ size_t compresskv_cache_evict_workspace_bytes(const ckv_cache *c, int32_t budget
  * more, the len - budget slots of the least accumulated weight go (ties: the
  * highest slots; NaN counts as less than any weight).  Slots of the first
  * n_sinks positions and of the last n_recent ones (>= seen - n_recent) go only
- * when no other is left.  The kept slots from budget on then move, in ascending
- * order, into the freed slots below it, in ascending order: rows, positions and
- * weights; no other slot is written.  Groups within the budget are left as they
- * are.  1 <= budget <= capacity; n_sinks, n_recent >= 0.
+ * when no other is left, the highest slots first.  The kept slots from budget on
+ * then move, in ascending order, into the freed slots below it, in ascending order:
+ * rows, positions and weights; no other slot is written.  Groups within the budget
+ * are left as they are.  1 <= budget <= capacity; n_sinks, n_recent >= 0.
  * ws: >= compresskv_cache_evict_workspace_bytes(), 256-byte aligned.
  */
 int compresskv_cache_evict(const ckv_cache *c, int32_t budget, int32_t n_sinks, int32_t n_recent,
@@ -166,12 +167,16 @@ size_t compresskv_window_attention_workspace_bytes(const ckv_window_problem *p);
  * of sequence b are its last Lq = cu_q[b+1] - cu_q[b] tokens: query i stands at
  * t = Lk - Lq + i (Lk = cu_k[b+1] - cu_k[b] keys) and sees the keys j <= t with
  * j > t - window or j < n_sinks.  So Lq = Lk is a prompt, 1 < Lq < Lk a chunk of
- * one, Lq = 1 a decoding step.  A query that sees nothing (t < 0) gives zeros.
+ * one, Lq = 1 a decoding step.  A query that sees nothing (t < 0) gives zeros, and
+ * so does one whose every visible logit is -infinity.
  * q [Tq][Hq][D], k, v [Tk][Hkv][D] packed, with the problem's strides; out
  * [Tq][Hq][D] dense; all 16-byte aligned.  Rows of out past the last sequence
- * are not written.  Sums and softmax are held in fp32; K and V of a key that a
- * query does not see do not reach it, whatever they hold.  Without any query
- * nothing is done, and q and out may be NULL; without any key k and v may be.
+ * are not written.  Logits, sums and softmax are held in fp32.  Before the product
+ * with V a bf16 call rounds a probability once more: to 16 bits where no sequence has
+ * more than 16 query rows per group (tokens times Hq / Hkv) or tokens of K or V lie more
+ * than 2^24 bytes apart, and otherwise to 8 bits, as the output (the error is then about
+ * 1.3 times that of the output's own rounding).  K and V of a key that a query does
+ * not see do not reach it, whatever they hold.  Without any query nothing is done, and q and out may be NULL; without any key k and v may be.
  * Refused besides: 2^31 query rows (tokens times Hq / Hkv) or more in one sequence, and
  * more than 2^24 - 512 blocks of query rows in all; a block is 128 rows (bf16, more than 16
  * rows in some sequence, and tokens of K and V at most 2^24 bytes apart) or else 16 or 32.

@@ -307,3 +307,22 @@ def test_a_row_that_is_not_a_number_gives_nothing_to_slots_it_does_not_see(gpu, 
         tol = (p * err).sum((0, 1)) + H.U * (12 * np.nan_to_num(want) + old + np.nan_to_num(want))
         assert (np.abs(weight[0, g, :n] - old - want) <= tol + 1e-30)[fine].all(), g
     assert np.isnan(H.values(out)[0, 0, 1]).all() and np.isfinite(H.values(out)[0, 1:]).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n_q", [1, 2])
+@pytest.mark.parametrize("cap", [80, 5000])
+def test_slots_of_logits_of_minus_infinity(gpu, dtype, n_q, cap):
+    """They receive nothing; where there are no others, the row gives zeros."""
+    cache = H.make_cache(C, dtype, [[cap, cap]], cap, 64, gpu, 66)
+    q = _rows((1, n_q, 4, 64), dtype, 67, gpu)
+    q[..., 0] = 1.0
+    cache.k[0, 0, :, 0] = -float("inf")
+    cache.k[0, 1, :cap - 9, 0] = -float("inf")
+    before = cache.weight.clone()
+    out = H.values(cache.attend(q, accumulate=True))
+    assert not out[0, :, :2].any() and (out[0, :, 2:] != 0).all()
+    assert (cache.weight[0, 0] == before[0, 0]).all()
+    assert (cache.weight[0, 1, :cap - 9] == before[0, 1, :cap - 9]).all()
+    received = (cache.weight - before)[0, 1, cap - 9:].double().sum().item()
+    assert abs(received - 2 * n_q) <= 2 * n_q * 9 * 2.0 ** -22   # 9 weights below 4, rounded

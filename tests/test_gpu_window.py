@@ -203,3 +203,31 @@ def test_a_long_prompt_beside_single_tokens(gpu, dtype, singles):
         back = min(at, window - 1)
         qs, ks = slice(singles + at, singles + at + 150), slice(tk - n + at - back, tk - n + at + 150)
         _check(q[qs], k[ks], v[ks], [(150, 150 + back)], window, 0, out[qs])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("spans,window", [([(1, 300), (1, 40)], 1 << 20), ([(4, 600), (2, 90)], 500),
+                                          ([(1, 6000)], 5000), ([(4, 5000), (0, 9), (3, 4000)], 1 << 20)],
+                         ids=["tokens", "drafts", "tokens-split", "drafts-split"])
+def test_probabilities_of_few_rows_keep_16_bits(gpu, d, spans, window):
+    """Up to 16 query rows per group: the output is off by its own rounding and little else."""
+    q, k, v, cu_q, cu_k = _inputs(spans, 8, 2, d, BF16, gpu, 18)
+    p = C.WindowProblem(q, k, v, cu_q, cu_k, window=window, n_sinks=4)
+    _check(q, k, v, spans, window, 4, C.window_attention(p, q, k, v), bits=16)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("lq,lk", [(1, 50), (1, 4000), (3, 60), (3, 4000), (150, 150), (150, 4000)])
+def test_logits_of_minus_infinity(gpu, dtype, lq, lk):
+    """A key whose logit is -infinity receives nothing; a row that sees no other gives zeros."""
+    q, k, v, cu_q, cu_k = _inputs([(lq, lk)], 4, 2, 64, dtype, gpu, 19)
+    q[:, :, 0] = 1.0                                          # every head: 1 * -infinity
+    hidden = lk - lq // 3 - 20                                # keys before it
+    k[:hidden, :, 0] = -float("inf")
+    p = C.WindowProblem(q, k, v, cu_q, cu_k, window=30)
+    out = C.window_attention(p, q, k, v)[:lq]
+    t = np.arange(lk - lq, lk)
+    assert not H.values(out)[t < hidden].any()
+    kept = torch.cat((k[hidden:lk], k[lk:])), torch.cat((v[hidden:lk], v[lk:]))
+    some = np.nonzero(t >= hidden)[0]
+    _check(q[some[0]:lq], *kept, [(len(some), lk - hidden)], 30, 0, out[some[0]:])
