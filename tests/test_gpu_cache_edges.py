@@ -326,3 +326,33 @@ def test_slots_of_logits_of_minus_infinity(gpu, dtype, n_q, cap):
     assert (cache.weight[0, 1, :cap - 9] == before[0, 1, :cap - 9]).all()
     received = (cache.weight - before)[0, 1, cap - 9:].double().sum().item()
     assert abs(received - 2 * n_q) <= 2 * n_q * 9 * 2.0 ** -22   # 9 weights below 4, rounded
+
+
+def test_the_most_groups_that_a_call_takes(gpu):
+    """65535 groups: a few of them give what they give in a small cache."""
+    n, cap, d = 65535, 32, 64
+    g = torch.Generator(device=gpu).manual_seed(68)
+    cache = C.Cache.empty(n, 1, cap, d, BF16, gpu)
+    cache.length.copy_(torch.randint(0, cap, (n, 1), generator=g, device=gpu))
+    cache.seen.copy_(cache.length)
+    cache.pos.copy_(torch.arange(cap, dtype=torch.int32, device=gpu).expand(n, 1, cap))
+    cache.weight.copy_(torch.rand((n, 1, cap), generator=g, device=gpu))
+    for t in (cache.k, cache.v):
+        t.copy_(torch.randn(t.shape, generator=g, device=gpu))
+    q = torch.randn((n, 1, 4, d), generator=g, device=gpu).to(BF16)
+    new = torch.randn((n, 1, 1, d), generator=g, device=gpu).to(BF16)
+    some = torch.tensor([0, 1, 255, 256, 32767, 32768, 65533, 65534], device=gpu)
+    small = C.Cache.empty(len(some), 1, cap, d, BF16, gpu)
+    for a, b in zip(small._tensors(), cache._tensors()):
+        if a is not None:
+            a.copy_(b[some])
+
+    def steps(cache, q, new):
+        cache.append(new, new)
+        out = cache.attend(q, accumulate=True)
+        cache.evict(20, n_sinks=2, n_recent=4)
+        return out, cache.read()[0]
+    for got, want in zip(steps(cache, q, new), steps(small, q[some], new[some])):
+        assert (H.bits(got[some]) == H.bits(want)).all()
+    assert (H.bits(cache.weight[some]) == H.bits(small.weight)).all()
+    assert int(cache.length.max()) == 20

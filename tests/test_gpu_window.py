@@ -231,3 +231,15 @@ def test_logits_of_minus_infinity(gpu, dtype, lq, lk):
     kept = torch.cat((k[hidden:lk], k[lk:])), torch.cat((v[hidden:lk], v[lk:]))
     some = np.nonzero(t >= hidden)[0]
     _check(q[some[0]:lq], *kept, [(len(some), lk - hidden)], 30, 0, out[some[0]:])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_window_attention_of_the_most_sequences(gpu, dtype):
+    rng = np.random.default_rng(20)
+    spans = [(0, 0)] * 65535
+    for s in [0, 63, 64, 1023, 1024, 65472, 65534, *rng.choice(65535, 40, replace=False)]:
+        spans[s] = (int(rng.integers(9, 40)),) * 2
+    q, k, v, cu_q, cu_k = _inputs(spans, 2, 1, 64, dtype, gpu, 21)
+    p = C.WindowProblem(q, k, v, cu_q, cu_k, window=20, n_sinks=2)
+    out = C.window_attention(p, q, k, v)
+    _check(q, k, v, [s for s in spans if s[0]], 20, 2, out)
