@@ -180,8 +180,7 @@ size_t compresskv_window_attention_workspace_bytes(const ckv_window_problem *p);
  * Refused besides: 2^31 query rows (tokens times Hq / Hkv) or more in one sequence, and
  * more than 2^24 - 512 blocks of query rows in all; a block is 128 rows (bf16, more than 16
  * rows in some sequence, and tokens of K and V at most 2^24 bytes apart) or else 16 or 32.
- * ws: >= compresskv_window_attention_workspace_bytes(), 256-byte aligned; none (256
- * bytes) where no row is split over workgroups.
+ * ws: >= compresskv_window_attention_workspace_bytes(), 256-byte aligned.
  */
 int compresskv_window_attention(const ckv_window_problem *p, const void *q, const void *k,
                                 const void *v, void *out, void *ws, size_t ws_bytes, void *stream);

@@ -52,8 +52,9 @@ constexpr int kJoinSlots = 1024;   // slots whose weights one workgroup adds to
 // parts, whose sums are added in order.  Each of the others adds to the
 // weights of kJoinSlots slots what the group's rows gave them, row by row in
 // order.  Bound by the latency of its few dependent loads, and with many rows by the
-// logits: 4.2 us for 128 groups in 4 splits, 4 rows of up to 4096 logits; 8.5 us for 64
-// groups in 8 splits, 28 rows of up to 3936 (24 MB).
+// logits: 4.3 us for 128 groups in 4 splits, 4 rows of up to 4096 logits; 9.3 us for 64
+// groups in 8 splits, 28 rows of up to 3936 (24 MB; 8.5 us without the comparison of
+// positions).
 template <AttendSource SRC, typename T, int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendArgs a, int out_blocks) {
   const int tid = threadIdx.x, bg = blockIdx.y, RM = 16 * a.rt;

@@ -1,4 +1,11 @@
 // Attention over f32 rows, of a cache or packed (attend_kernels.h).
+//
+// Windowed prompts and chunks run here too, 32 rows per workgroup.  They share no tile: each
+// wave reads its own K and V rows from the caches, a key again for every 32 rows (6.4 GB and
+// 8.8 GB in the first and the last call below).  32 / 8
+// heads, D = 128, against the fp32 products alone (a library product reaches 153
+// TFLOP/s): 4 prompts of 2048 tokens, 1024 keys, 1112 us against 676; a chunk of 1024 over
+// 8192 keys 190 against 113; a prompt of 32768 tokens, 256 keys, 1990 against 909.
 #include "attend_kernels.h"
 
 namespace ckv {

@@ -25,13 +25,17 @@
 // waits for memory, so the second product costs nothing and the output is rounded
 // once, at its end.
 //
-// Bound by memory, and in short calls by the chain of a few dependent loads (length,
-// rows, the waves' join).  Measured, D = 128, 32 / 8 heads: 16 caches of up to 4096 4-bit
-// slots 17.5 us for 50 MB (2.9 TB/s; a copy reaches 4.9, a read 5.8), of which about
-// 5 us are start and join; 8 of up to 131072, 28 / 4 heads, 97-99 us for 496 MB (5.0
-// TB/s); four tokens over 16 caches of up to 3936 bf16 slots 28.3 us for 114 MB of rows
-// and 24 MB of logits; one cache of 1001 4-bit slots 9.3 us; single tokens in
-// windows of 1028 keys, 256 groups of bf16, 23.6 us for 134 MB (5.7 TB/s).
+// Bound by memory where the rows are many: 8 caches of up to 131072 4-bit slots, D = 128,
+// 28 / 4 heads, 98 us for 496 MB (5.0 TB/s; a copy reaches 4.9, a read 5.8), the CUs busy for
+// 80% of the cycles, the vector pipe (which widens the rows) for 46%, the matrix pipe for
+// 18%; single tokens in windows of 1028 keys, 256 groups of bf16, 24 us for 134 MB (5.6
+// TB/s); four tokens over 16 caches of up to 3936 bf16 slots 29 us for 114 MB of rows and
+// 24 MB of logits.  Shorter calls wait: for the chain of a few dependent loads
+// (length, rows, the waves' join), and for the longest group, as every group has the same
+// number of splits.  16 caches of up to 4096 4-bit slots, 32 / 8 heads, 17.3 us for 50 MB (2.9
+// TB/s): CUs busy for 49%, vector pipe 22%, matrix pipe 7%.  The whole call with as many
+// slots in all, uneven (a third of 4096 to all) and even: 16 caches 21.8 and 18.9 us,
+// 64 caches 43.3 and 33.3 us.  One cache of 1001 slots 9.2 us.
 #pragma once
 
 #include "attend.h"

@@ -14,11 +14,14 @@
 // P is rounded to bf16 once (2^-8 of each probability, as the output itself);
 // its sum is taken before that, in fp32.
 //
-// 32 / 8 heads, D = 128: a prompt of 32768 tokens under a window of 4096 keys 2.12-2.20 ms,
-// 940-975 TFLOP/s of the products that its visible pairs need, where a library product of
-// 8192^3 reaches 1240; 8 prompts of 4096 to 16384 tokens under 1024 keys 1.63-1.67 ms,
-// 805-825 TFLOP/s (the tiles at both ends of a window of 1024 are a tenth more).  The matrix
-// pipe is busy for 45% of the cycles and the vector one for 43%: two waves per SIMD
+// 32 / 8 heads, D = 128 (medians): a prompt of 32768 tokens under a window of 4096 keys 2.22 ms,
+// 930 TFLOP/s of the products that its visible pairs need, where a library product of
+// 8192^3 reaches 1240; 8 prompts of 4096 to 16384 tokens under 1024 keys 1.69 ms,
+// 797 TFLOP/s (the tiles at both ends of a window of 1024 are a tenth more).  Narrow windows
+// leave few tiles to a row block, and its first load, masks and output uncovered: 8 prompts of
+// 4096 tokens under 1024, 512, 256, 128, 32 keys 631, 405, 284, 220, 187 us, where the
+// products and the bytes take 389, 209, 116, 116, 116.  The matrix
+// pipe is busy for 45% of the cycles and the vector one for 45%: two waves per SIMD
 // overlap the softmax of one with the products of the other by chance alone.  (One wave that
 // works on the softmax of a tile between the products of its neighbours took 2480 us:
 // its registers did not hold both.)
