@@ -43,3 +43,12 @@ def test_srh_score_issues_a_batch_of_span_loads_together():
     before = body[:body.index("v_cvt_f64_f32")]
     run = re.split(r"^(?:\S+:|\s+s_c?branch\S*|\s+s_\w*saveexec\S*)", before, flags=re.M)[-1]
     assert len(re.findall(r"^\s+global_load_dword\s", run, re.M)) == batch
+
+
+def test_two_waves_per_simd_of_windowed_fp32_prompts():
+    """512 registers / 2, and nothing in scratch: with one wave, prompts take 1.3 times as long.
+    (The search for a workgroup's sequence can cost the second one.)"""
+    _, vgprs, agprs, scratch, _ = _resources(
+        "attend_f32.hip", "attend_kernelILNS_12AttendSourceE1ELNS_9CacheTypeE0ELi128ELi2ELi1ELb1ELb0E")
+    assert vgprs + agprs <= 256
+    assert scratch == 0
