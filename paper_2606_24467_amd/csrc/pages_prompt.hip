@@ -107,7 +107,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void pages_prompt_kernel(
 
   // The pages of 64 segments, of those before and of those after them, in LDS: window w holds the
   // segments tile0 SEGS + 64 w .., and is loaded 16 tiles ahead.  (In registers they would make the first look
-  // at them wait for the rows that are under way.)
+  // at them wait for the rows that are under way.)  The wave that loads one waits for it before the next
+  // tile's barrier (arrive), the others read it behind that.
   constexpr int kWindow = 64 / SEGS;             // tiles of a window
   __shared__ __align__(16) int page_s[4][64];
   const int segments = (n + 15) / 16;
@@ -226,15 +227,16 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void pages_prompt_kernel(
       *reinterpret_cast<uint4 *>(to + b_row * RB + 16 * ((4 * b_of + u) ^ swizzle)) = x;
     }
   };
-  // Waits for this wave's loads, of K to k (if `more`) and of V to v (8-bit: widens them).
+  // Waits for this wave's loads, of K to k (if `more`) and of V to v (8-bit: widens them), and of page
+  // numbers.  Every wave waits, those too that have no rows of 8 bits to widen: the barrier behind this
+  // does not order their loads to LDS before the other waves' reads.
   auto arrive = [&](char *k, char *v, bool more) __attribute__((always_inline)) {
-    if constexpr (!FP8) {
-      __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0)
-    } else if constexpr (BOTH) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);          // vmcnt(0)
+    if constexpr (FP8 && BOTH) {
       if (more) widen(k, 0, swizzle_k(b_row));
       widen(v, 1, swizzle_v(b_row));
-    } else if (has && (is_v || more)) {
-      widen(is_v ? v : k, 0, is_v ? swizzle_v(b_row) : swizzle_k(b_row));
+    } else if constexpr (FP8) {
+      if (has && (is_v || more)) widen(is_v ? v : k, 0, is_v ? swizzle_v(b_row) : swizzle_k(b_row));
     }
   };
 
