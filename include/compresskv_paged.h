@@ -163,8 +163,10 @@ size_t compresskv_paged_attend_workspace_bytes(const ckv_paged_cache *c, const c
  * Before the product with V a bf16 call rounds a probability once more: to 16 bits in
  * sequences of at most 32 query rows per group (tokens times Hq / Hkv), and to 8 bits, as the
  * output, in others.  The products with V are added up before they are divided by the sum, so
- * that values of V beyond 2^116 / (keys seen) may give infinities.  K and V of keys that a row
- * does not see do not reach it, whatever they hold.
+ * that values of V beyond 2^116 / (keys seen) may give infinities.  An infinite value of V
+ * whose key has a weight of 2^-100 of the row's largest at least gives that infinity (NaN where both
+ * signs meet); one of less weight may give a NaN instead.  K and V of keys that a row does not see
+ * do not reach it, whatever they hold.
  * Refused besides: 2^31 query rows (tokens times Hq / Hkv) or more in one sequence, and
  * more than 2^23 - 4096 blocks of query rows in all.  A block is 256 rows of a bf16 sequence
  * (128 where none has more), and 32 of one of at most 32 rows and of fp32 (16 where none has more than 16,

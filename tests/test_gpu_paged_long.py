@@ -232,3 +232,29 @@ def test_values_that_are_not_finite_in_long_chunks(gpu, kind, m, d):
     out = cache.attend(PH.chunk_of(C, [m] * batch, gpu), q)
     _check(cache, [m] * batch, q, out, 1.0 / np.sqrt(d))
     assert torch.isfinite(out[0, :, 33:d - 1]).all()          # its row sees none of these
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("m", [1, 12, 40], ids=["8rows", "96rows", "320rows"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_infinite_values_of_little_weight(gpu, dtype, m, d):
+    """A visible infinity with a weight of 2^-100 of the row's largest, or more, is one in the output,
+    wherever its key lies."""
+    _say("little weight", dtype, m, d)
+    batch, n, hq, hkv = 24, 2500, 16, 2
+    lengths = [n - 3 * b for b in range(batch)]
+    cache = _cache(dtype, lengths, hkv, d, gpu, 41)
+    cache.k[..., 0] = 0.0
+    table = cache.page_table.cpu().numpy()
+    for b, n in enumerate(lengths):
+        j = (3, n // 2, 110 * b, n - m, n - 1)[b % 5]
+        page, slot = int(table[b, j // 16]), j % 16
+        cache.k[page, :, slot] = 0.0
+        cache.k[page, :, slot, 0] = -64.0
+        cache.v[page, :, slot, 5] = torch.inf if b % 2 else -torch.inf
+    q = _randn((m * batch, hq, d), dtype, gpu, 42) / 32
+    q[..., 0] = 1.0
+    # the largest other logit is below 69.3 - 64: 5 is 20 deviations of one, at d = 128 14
+    out = cache.attend(PH.chunk_of(C, [m] * batch, gpu), q, scale=1.0)
+    _check(cache, [m] * batch, q, out, 1.0)
+    assert torch.isinf(out.reshape(batch, m, hq, d)[:, -1, :, 5]).all()
