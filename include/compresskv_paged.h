@@ -76,8 +76,9 @@ typedef struct ckv_rows {
  * Rotates the rows of n_tokens >= 0 tokens: n_q_heads >= 0 heads of q to q_out and
  * n_k_heads >= 0 of k to k_out, at least one head in all (q, k: input rows, only
  * read).  pos: int32 [n_tokens], any values.  transposed: 0, or 1 for the transposed
- * rotation, which takes the gradient of an output to that of its input.  An
- * output is rounded to its type once.  dtype: CKV_F32 or CKV_BF16.  Outputs may be their
+ * rotation, which takes the gradient of an output to that of its input.  Values are computed in
+ * fp32, from cosines and sines that are rounded to it once: off by 2^-22 (|x0 c| + |x1 s|) at most, besides
+ * what the table's angles are.  A bf16 output is rounded once more.  dtype: CKV_F32 or CKV_BF16.  Outputs may be their
  * own inputs (same data and strides) and must not overlap otherwise.
  */
 int compresskv_rotary(const ckv_rotary *r, int32_t dtype, int32_t transposed, int32_t n_tokens,
@@ -119,9 +120,9 @@ typedef struct ckv_chunk {
  * ones goes to position len[b] - n + i (positions below 0 are not written).
  * r: NULL, or the rotation of k_new (and of q, if n_q_heads > 0, to q_out), by that
  * position.  k_new, v_new, q: rows of dtype CKV_F32 or CKV_BF16 (the cache's own unless it is
- * CKV_FP8).  Without a rotation n_q_heads is 0.  An output or stored value is rounded
- * once, from 32 bits; an 8-bit one from 64 (so that the code is the nearest).  q_out may be q
- * itself.
+ * CKV_FP8).  Without a rotation n_q_heads is 0.  q_out and rows stored in fp32 or bf16 are as
+ * compresskv_rotary gives them; 8-bit rows are turned in fp64, so that a code is the nearest to the exact
+ * value.  q_out may be q itself.
  */
 int compresskv_paged_append(const ckv_paged_cache *c, const ckv_chunk *ch, const ckv_rotary *r,
                             int32_t dtype, const ckv_rows *k_new, const ckv_rows *v_new,
