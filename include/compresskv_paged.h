@@ -151,6 +151,9 @@ typedef struct ckv_paged_attend_problem {
   int32_t reserved[2];  /* must be 0 */
 } ckv_paged_attend_problem;
 
+/* Bytes of workspace, by the chunk's tokens, the heads and max_len: what the splits of the keys need that
+ * the lengths may make, 165 MiB at most (single tokens of 8 groups: 2 MiB; a chunk of 2048 tokens
+ * of 8 groups of 4 heads of 128: 98 MiB).  Calls that follow each other on a stream can share one. */
 size_t compresskv_paged_attend_workspace_bytes(const ckv_paged_cache *c, const ckv_chunk *ch,
                                                const ckv_paged_attend_problem *p);
 

@@ -305,13 +305,14 @@ int plan_pages(const ckv_paged_cache *c, const ckv_chunk *ch, const ckv_paged_at
     if (all_blocks > kMaxBlocks) return fail(CKV_UNSUPPORTED, "too many query rows for one launch");
     a.blocks = (int32_t)blocks;
     // A sequence is split where it has more keys than all blocks' keys / target, so that one with
-    // `target` blocks never is.  The splits are then blocks + target at most, those of blocks of
-    // several 2 target, and such blocks target.
+    // `target` blocks never is, and blocks that are split are fewer than `target`.  A block's splits are
+    // less than one more than its keys over those, so that all blocks have blocks + target at most, and
+    // those that are split as many as they are + target.
     const int64_t most_splits = (a.max_len + a.least - 1) / a.least;
     if (most_splits == 1) may_split = 0;
     a.grid = (int32_t)(blocks + std::min<int64_t>(may_split * (most_splits - 1), may_split ? a.target : 0));
     a.joins = (int32_t)std::min<int64_t>(may_split, a.target);
-    const size_t parts = (size_t)std::min<int64_t>(may_split * most_splits, 2 * a.target) * a.part_rows;
+    const size_t parts = (size_t)std::min<int64_t>(may_split * most_splits, a.joins + a.target) * a.part_rows;
     la.at = pl.total;
     la.ml_bytes = round_up(parts * sizeof(float2), 256);
     la.o_bytes = round_up(parts * c->head_dim * sizeof(float), 256);
