@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_api.h"
 #include "pages_attend.h"
@@ -18,7 +19,8 @@ struct PagesBoth {
   PagesArgs a[2];
 };
 
-// One of the two, in the kernel's arguments (which selected by a value of theirs would be copied).
+// One of the two, in the kernel's arguments (which selected by a value of theirs would be copied).  They
+// are the kernel's first argument, which lies at the start of them.
 __device__ __forceinline__ const PagesArgs &pages_args(int which) {
   typedef const __attribute__((address_space(4))) PagesBoth *kernarg_ptr;
   return ((const PagesBoth *)(kernarg_ptr)__builtin_amdgcn_kernarg_segment_ptr())->a[which];
@@ -84,6 +86,10 @@ __global__ __launch_bounds__(1024) void pages_index_kernel(const PagesArgs a) { 
 __global__ __launch_bounds__(1024) void pages_index_both_kernel(const PagesBoth) {
   pages_index(pages_args(blockIdx.x));
 }
+
+template <typename First, typename... Rest>
+std::is_same<First, PagesBoth> both_come_first(void (*)(First, Rest...));
+static_assert(decltype(both_come_first(pages_index_both_kernel))::value);
 
 // Grid (blocks of several splits, a few workgroups for the rows of each), 256 threads: D / 4 lanes per
 // row, and where that leaves lanes (few rows, many splits) the splits are dealt to several such
@@ -155,6 +161,8 @@ __global__ __launch_bounds__(256) void pages_join_both_kernel(const PagesBoth, i
   const int which = (int)blockIdx.x >= first_joins ? 1 : 0;     // uniform
   pages_join<T, D>(pages_args(which), (int)blockIdx.x - which * first_joins);
 }
+
+static_assert(decltype(both_come_first(pages_join_both_kernel<float, 64>))::value);
 
 void launch_pages_join(PagesBoth &both, bool f32, int head_dim, hipStream_t stream) {
   const int joins = both.a[0].joins + both.a[1].joins;
