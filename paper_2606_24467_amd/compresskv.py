@@ -1134,11 +1134,12 @@ class Rotary:
                  base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0,
                  low: float = 1.0, high: float = 4.0, original_len: int = 8192,
                  amplitude: float = 1.0, inv_freq=None, device):
+        head_dim, layout = _int32(head_dim, "head_dim"), _int32(layout, "layout")
         rotary_dim = head_dim if rotary_dim is None else _int32(rotary_dim, "rotary_dim")
         turns = np.zeros(max(0, rotary_dim // 2), dtype=np.uint64)
         if inv_freq is None or rotary_dim < 16 or rotary_dim > 128 or rotary_dim % 16:
             _check("compresskv_rotary_turns", lib().compresskv_rotary_turns(
-                rotary_dim, float(base), int(scaling), float(factor), float(low), float(high),
+                rotary_dim, float(base), _int32(scaling, "scaling"), float(factor), float(low), float(high),
                 _int32(original_len, "original_len"), turns.ctypes.data))
         else:
             f = np.asarray(inv_freq.cpu() if isinstance(inv_freq, torch.Tensor) else inv_freq,
