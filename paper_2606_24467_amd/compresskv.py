@@ -3,7 +3,9 @@
 The functions mirror the C ABI in include/compresskv.h,
 include/compresskv_offline.h, include/compresskv_cache.h and
 include/compresskv_paged.h and take torch tensors for device memory; every computation runs in the HIP library.  There is no
-fallback: if the library is missing or fails to load, every call raises.
+fallback: if the library is missing or fails to load, every call raises.  No call
+records a gradient: outputs do not require one, whatever the inputs do (a rotation's gradient
+is its transposed rotation).
 """
 from __future__ import annotations
 
@@ -1383,7 +1385,8 @@ class PagedCache:
                out=None, ws=None, stream=None):
         """Causal attention of the chunk's q [T, Hq, D], D contiguous, over the pages, the chunk's
         own rows among them; returns out [T, Hq, D].  max_len: no sequence is longer (default:
-        max_pages * page_size)."""
+        max_pages * page_size).  ws: a workspace, which calls that follow each other on a stream can
+        share; without one each call allocates its own (up to 165 MiB)."""
         index = self._index
         key = (q.shape, q.stride(), q.dtype, chunk.tokens, chunk.batch, scale, max_len)
         known = self._attends.get(key)

@@ -292,6 +292,9 @@ int plan_pages(const ckv_paged_cache *c, const ckv_chunk *ch, const ckv_paged_at
       return fail(CKV_UNSUPPORTED, "a sequence has 2^31 or more query rows per group");
     if (max_rows == 0) continue;
     ++pl.launches;
+    // Two row tiles where there are the rows for them.  fp32 queries over 8-bit rows take one: their three parts
+    // do not leave the registers for two (64 sequences of up to 8 new tokens over up to 4096 97 us, with two
+    // 202; four chunks of up to 750 tokens over up to 3000, 32 / 8 heads, D = 128: 305 and 458 us).
     if (c->dtype == p->dtype || p->dtype == CKV_BF16) la.rt = max_rows > 16 ? 2 : 1;
     const int rm = !la.prompt ? 16 * la.rt : max_rows > 128 ? 256 : 128;
     a.rm_log2 = __builtin_ctz(rm);

@@ -7,7 +7,9 @@
 // instruction: lane 32 h + c holds query row c against the keys 8 (i / 4) + 4 h + i % 4 of 32
 // (element i), which is the order of the reduction slots that P^T goes into the second product
 // with, if V comes in the same order; the transposing LDS read gives it so.  P never leaves the
-// registers.  It is rounded to bf16 once; its sum is taken before that, in fp32.
+// registers.  It is rounded to bf16 once, and its sum is taken before that, in fp32: a second part
+// of it would be a third product beside two on the pipe that bounds the kernel, where the output is rounded
+// to bf16 as well (it is off by 0.0023 of exact arithmetic, where rounding the exact one gives 0.0017).
 //
 // A wave's matrix and vector work overlap: in one step it takes the logits of the 32 keys to come,
 // the exponentials of 32 and the second product of the 32 before, none of which needs another, and
@@ -375,7 +377,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void pages_prompt_kernel(
     settle(s, sum[0] + sum[1], p);
   };
 
-  // The walk.  When a tile's turn comes, p holds the exponentials of its first half and `next` the
+  // The walk.  A segment without a page ends the fast loop: the split's tiles from there on go through the
+  // one with masks (2048 tokens over 32768 bf16 keys 1007 us, with a page missing in the middle 1313, with the
+  // first one missing 1641; 8-bit keys 1049 and, the first one, 1817).
+  // When a tile's turn comes, p holds the exponentials of its first half and `next` the
   // logits of its second; afterwards they hold the next tile's.
   f32x16 s, next;
   bf16x8 p[2];

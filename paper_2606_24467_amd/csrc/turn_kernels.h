@@ -11,10 +11,11 @@
 //
 // Bound by memory: each row is read and written once, and a token's cosines and sines are computed by
 // the lanes of its wave, so that no table of them is read.  32768 tokens of 32 + 8 heads of 128 bf16
-// values: 128 us, 671 MB at 5.2 TB/s (a large copy reaches 5.1); 64 tokens: 4.0 us, a launch; 5001
-// tokens of 8 + 2 heads of 64 fp32 values: 8.7 us, 26 MB at 2.9 TB/s, the start and the angles'
-// chain.  (The first rows loaded before the angles too: more registers, 4931 tokens into 8-bit pages
-// and back 69 -> 79 us.)
+// values: 128 us, 671 MB at 5.2 TB/s (a large read reaches 5.8); 64 tokens: 4.0 us, a launch; 5001
+// tokens of 8 + 2 heads of 64 fp32 values: 8.3 us, 26 MB at 3.1 TB/s, the start and the angles'
+// chain; 2048 tokens of 32 + 8 heads into bf16 pages 12.9 us, into fp32 ones 18.7, fp32 rows into 8-bit ones
+// 19.8.  (In the form for 8-bit pages the first rows were loaded before the angles too: more registers, 4931
+// tokens in and read back 69 -> 79 us.  The other forms were not measured so.)
 #pragma once
 
 #include <type_traits>
